@@ -274,6 +274,85 @@ dam_status_t dam_decode_attention(const void* q, const void* K, const void* V, c
                                   size_t scratch_bytes, void* stream);
 
 /*
+ * A KV cache held in 8 bits. Every value is code * scale, with one float scale for each block of block_tokens tokens and KV
+ * head, K and V apart (the paper has no counterpart; its generation reads a cache, and this one has half the bytes).
+ *   INT8  codes -127 .. 127; scale = amax / 127 (IEEE single division), code = the integer nearest to value / scale, ties to even
+ *   E4M3  8-bit floating point codes (largest 448); scale = the least power of two with amax <= 448 * scale,
+ *         code = value / scale rounded to nearest, ties to even
+ * amax is the largest magnitude of the block's tokens; no scale is below 2^-126. A block that holds an infinity or a NaN has
+ * the scale NaN, and its tokens read back as NaN, until its first token is written anew.
+ */
+typedef enum dam_code_t { DAM_CODE_INT8 = 0, DAM_CODE_E4M3 = 1 } dam_code_t;
+
+typedef struct dam_cache_t {
+  uint32_t struct_size;           /* sizeof(dam_cache_t)                                            */
+  int32_t num_seqs;               /* B >= 1                                                        */
+  const int32_t* cu_seqlens_host; /* HOST, B + 1 entries: sequence b has room for the tokens        */
+  const int32_t* cu_seqlens_dev;  /*   cu[b] .. cu[b+1] - 1; DEVICE, same values                    */
+  int32_t total_tokens;           /* = cu_seqlens[B], at most 2^31 - 256                            */
+  int32_t num_kv_heads;           /* Hkv                                                           */
+  int32_t head_dim;               /* 64 or 128                                                     */
+  int32_t code;                   /* dam_code_t                                                    */
+  int32_t block_tokens;           /* 16, 32, 64 or 128; block j of a sequence: its tokens j * block_tokens ... */
+  int32_t reserved;               /* 0                                                             */
+  void* k_codes;                  /* DEVICE, one byte per element, [total_tokens, Hkv, head_dim] by the strides */
+  void* v_codes;
+  float* k_scales;                /* DEVICE, [scale rows, Hkv]: block j of sequence b in row        */
+  float* v_scales;                /*   cu[b] / block_tokens + b + j (dam_cache_sizes: how many rows) */
+  int64_t k_stride_tok, k_stride_head; /* bytes, multiples of 16, head_dim contiguous               */
+  int64_t v_stride_tok, v_stride_head;
+} dam_cache_t;
+
+/*
+ * Sizes for one cache (host only; the code and scale pointers are not looked at and may be NULL): rows of k_scales and v_scales,
+ * and bytes of the scratch dam_cache_decode_attention wants for num_q_heads query heads (a multiple of num_kv_heads).
+ * Outputs (HOST pointers) may be NULL. Errors: INVALID_ARGUMENT, UNSUPPORTED (head_dim).
+ */
+dam_status_t dam_cache_sizes(const dam_cache_t* cache, int32_t num_q_heads, size_t* scale_rows, size_t* scratch_bytes);
+
+/*
+ * Writes new tokens into the cache: the packed K, V rows that `tokens` describes (its cu_seqlens say how many each sequence
+ * gets, 0 allowed; its K / V strides and dtype are used, num_seqs, num_kv_heads and head_dim are the cache's) become the
+ * tokens starts[b], starts[b] + 1, ... of sequence b. Prompts, chunks and single tokens go through the same call; the starts are
+ * read on the device, so that a captured call follows them.
+ * A block whose first token is among the new ones gets its scale from the new ones. A block that was begun before keeps its
+ * scale, or gets the larger one that its new tokens want; then the tokens that stand before starts[b] in it are read back (a
+ * float) and quantised again. Tokens behind the last new one are left as they are: they no longer belong to the sequence.
+ *   K, V    : DEVICE, 16-byte aligned.   starts_dev : DEVICE, int32[num_seqs], or NULL: every sequence from token 0.
+ *   scratch : DEVICE, >= 256 bytes, 256-byte aligned. A sequence whose tokens do not fit its capacity (starts[b] < 0 or
+ *             starts[b] + tokens > capacity) is left alone and gives INVALID_ARGUMENT in the status word.
+ * The new rows must not lie inside the cache. Errors: INVALID_ARGUMENT, UNSUPPORTED (head_dim), BUFFER_TOO_SMALL, CUDA.
+ */
+dam_status_t dam_cache_write(const void* K, const void* V, const dam_shape_t* tokens, const int32_t* starts_dev,
+                             const dam_cache_t* cache, void* scratch, size_t scratch_bytes, void* stream);
+
+/*
+ * Reads tokens back: the tokens starts[b] ... of every sequence, as many as `tokens` says, into the packed K, V rows it
+ * describes: code * scale, rounded to its dtype. With starts NULL and the lengths of a prompt this gives the K and V that
+ * dam_sparse_attention and dam_sparse_attention_rows take (a chunk of a prompt against what the cache holds).
+ * Arguments and errors as dam_cache_write; the rows of a sequence whose range does not fit become zeros.
+ */
+dam_status_t dam_cache_read(const dam_cache_t* cache, const dam_shape_t* tokens, const int32_t* starts_dev, void* K, void* V,
+                            void* scratch, size_t scratch_bytes, void* stream);
+
+/*
+ * Generation over the cache: the query of sequence b at position i = positions[b] attends to the keys 0..i of its sequence
+ * (mask == NULL), or to those of them that the patterns of a blob keep, exactly as dam_decode_attention chooses them.
+ *   q, O : DEVICE, [num_seqs, num_q_heads, head_dim] contiguous, 16-byte aligned, of type `dtype` (dam_dtype_t).
+ *   mask : DEVICE, NULL or a blob built for the same number of sequences and query heads (any lengths).
+ *   positions_dev : DEVICE, int32[num_seqs], 0 <= positions[b] < capacity of b (checked on the device: a violation gives
+ *          O = 0, LSE = -inf for that sequence and INVALID_ARGUMENT in the status word of `scratch`).
+ *   lse  : DEVICE, float[num_seqs, num_q_heads]; a query without a key gives O = 0, LSE = -inf.
+ *   scratch : DEVICE, >= the scratch bytes of dam_cache_sizes, 256-byte aligned; one call at a time.
+ * Tokens 0..i must have been written; codes behind them may hold anything, an E4M3 NaN code (0x7F, 0xFF) included, but no
+ * written token has one. num_q_heads must be a multiple of the cache's num_kv_heads; softmax_scale 0 selects
+ * 1 / sqrt(head_dim). Errors: INVALID_ARGUMENT, UNSUPPORTED (head_dim), BUFFER_TOO_SMALL, CUDA.
+ */
+dam_status_t dam_cache_decode_attention(const void* q, const dam_cache_t* cache, const void* mask, const int32_t* positions_dev,
+                                        int32_t num_q_heads, int32_t dtype, float softmax_scale, void* O, float* lse,
+                                        void* scratch, size_t scratch_bytes, void* stream);
+
+/*
  * Counts taken from a mask blob (DEVICE): out[0] = listed tiles (what the attention kernel executes; the
  * tensor-core kernel multiplies fewer where a head's single far diagonal lies across two tiles that hold nothing else),
  * out[1] = of those, fully active ones, out[2] = total causal tiles of the shape (for densities),

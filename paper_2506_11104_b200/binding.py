@@ -25,7 +25,7 @@ EXPORTS = ["dam_version", "dam_status_string", "dam_mask_sizes", "dam_build_mask
            "dam_mask_all_ones", "dam_sparse_attention", "dam_mask_stats", "dam_mask_expand_rows", "dam_poll_status",
            "dam_prefill_host", "dam_build_masks_static", "dam_static_scratch_bytes", "dam_selftest_bounded_wait",
            "dam_decode_attention", "dam_sparse_attention_rows", "dam_capture_accumulate", "dam_capture_average",
-           "dam_selftest_device_table"]
+           "dam_selftest_device_table", "dam_cache_sizes", "dam_cache_write", "dam_cache_read", "dam_cache_decode_attention"]
 
 
 class DamError(RuntimeError):
@@ -46,6 +46,17 @@ class dam_shape_t(ctypes.Structure):
                 ("o_stride_tok", ctypes.c_int64), ("o_stride_head", ctypes.c_int64)]
 
 
+class dam_cache_t(ctypes.Structure):
+    _fields_ = [("struct_size", ctypes.c_uint32), ("num_seqs", ctypes.c_int32),
+                ("cu_seqlens_host", ctypes.c_void_p), ("cu_seqlens_dev", ctypes.c_void_p),
+                ("total_tokens", ctypes.c_int32), ("num_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("code", ctypes.c_int32), ("block_tokens", ctypes.c_int32), ("reserved", ctypes.c_int32),
+                ("k_codes", ctypes.c_void_p), ("v_codes", ctypes.c_void_p),
+                ("k_scales", ctypes.c_void_p), ("v_scales", ctypes.c_void_p),
+                ("k_stride_tok", ctypes.c_int64), ("k_stride_head", ctypes.c_int64),
+                ("v_stride_tok", ctypes.c_int64), ("v_stride_head", ctypes.c_int64)]
+
+
 class dam_rule_t(ctypes.Structure):
     _fields_ = [("struct_size", ctypes.c_uint32), ("pcl_max", ctypes.c_int32), ("tau", ctypes.c_float),
                 ("mu", ctypes.c_float), ("lambda_", ctypes.c_float), ("eps", ctypes.c_float),
@@ -64,7 +75,9 @@ _ARGS = {"dam_status_string": "i", "dam_mask_sizes": "ppippp", "dam_build_masks"
          "dam_mask_stats": "ppppp", "dam_mask_expand_rows": "ppiiiiipp", "dam_poll_status": "pp",
          "dam_prefill_host": "pppppippppp", "dam_build_masks_static": "pppppzp", "dam_selftest_bounded_wait": "pzup",
          "dam_decode_attention": "ppppppifpppzp", "dam_sparse_attention_rows": "pppppiifpppppzp",
-         "dam_capture_accumulate": "ppippp", "dam_capture_average": "ppifppp", "dam_selftest_device_table": "pipp"}
+         "dam_capture_accumulate": "ppippp", "dam_capture_average": "ppifppp", "dam_selftest_device_table": "pipp",
+         "dam_cache_sizes": "pipp", "dam_cache_write": "ppppppzp", "dam_cache_read": "ppppppzp",
+         "dam_cache_decode_attention": "ppppiifpppzp"}
 _CTYPE = {"p": ctypes.c_void_p, "z": ctypes.c_size_t, "i": ctypes.c_int32, "u": ctypes.c_uint32, "f": ctypes.c_float}
 
 _lib = None
@@ -332,6 +345,125 @@ def dam_decode_attention(q, K, V, mask, shape: Shape, positions: torch.Tensor, s
                                     Hq // shape.c.num_kv_heads, softmax_scale, _ptr(O), _ptr(lse),
                                     _ptr(scratch), scratch.numel(), _stream(q.device))
     _check(rc, "dam_decode_attention")
+    return O, lse, scratch
+
+
+CACHE_CODES = {"int8": (0, torch.int8), "e4m3": (1, torch.float8_e4m3fn)}
+
+
+@dataclass
+class Cache:
+    """Python-side owner of a dam_cache_t and the buffers it points to."""
+    c: dam_cache_t
+    cu_host: np.ndarray
+    cu_dev: Optional[torch.Tensor]
+    lengths: List[int]
+    k_codes: Optional[torch.Tensor]
+    v_codes: Optional[torch.Tensor]
+    k_scales: Optional[torch.Tensor]
+    v_scales: Optional[torch.Tensor]
+
+    @property
+    def ref(self):
+        return ctypes.byref(self.c)
+
+
+def make_cache(cu_seqlens: Sequence[int], Hkv: int, d: int, code: str = "int8", block_tokens: int = 64, device=None,
+               k_codes: Optional[torch.Tensor] = None, v_codes: Optional[torch.Tensor] = None,
+               k_scales: Optional[torch.Tensor] = None, v_scales: Optional[torch.Tensor] = None) -> Cache:
+    """A KV cache held in 8 bits, with room for cu_seqlens[b + 1] - cu_seqlens[b] tokens of sequence b.
+
+    Buffers that are not given are allocated on `device` (zeros); codes [tokens, Hkv, d] of one byte, any strides with the
+    last dimension contiguous; scales fp32 [rows, Hkv], contiguous.  Without a device: a description for host-only calls."""
+    cu_host = np.ascontiguousarray(cu_seqlens, dtype=np.int32)
+    lengths = [int(b - a) for a, b in zip(cu_host[:-1], cu_host[1:])]
+    T, (number, dtype) = int(cu_host[-1]), CACHE_CODES[code]
+    c = dam_cache_t()
+    c.struct_size = ctypes.sizeof(dam_cache_t)
+    c.num_seqs, c.total_tokens, c.num_kv_heads, c.head_dim = len(lengths), T, Hkv, d
+    c.code, c.block_tokens = number, block_tokens
+    c.cu_seqlens_host = cu_host.ctypes.data
+    cu_dev = None
+    codes, scales = [k_codes, v_codes], [k_scales, v_scales]
+    if device is None:
+        c.cu_seqlens_dev = 1                                  # non-null placeholder for host-only calls
+    else:
+        cu_dev = torch.from_numpy(cu_host.copy()).to(device)
+        c.cu_seqlens_dev = cu_dev.data_ptr()
+        rows = T // block_tokens + len(lengths)
+        codes = [torch.zeros(T, Hkv, d, dtype=dtype, device=device) if x is None else x for x in codes]
+        scales = [torch.zeros(rows, Hkv, dtype=torch.float32, device=device) if x is None else x for x in scales]
+        for x in codes:
+            assert x.element_size() == 1 and x.shape == (T, Hkv, d) and (x.stride(2) == 1 or x.numel() == 0)
+        for x in scales:
+            assert x.dtype == torch.float32 and x.is_contiguous() and x.numel() >= rows * Hkv
+        (c.k_codes, c.v_codes), (c.k_scales, c.v_scales) = map(_ptr, codes), map(_ptr, scales)
+    (c.k_stride_tok, c.k_stride_head), (c.v_stride_tok, c.v_stride_head) = (
+        (Hkv * d, d) if x is None or x.numel() == 0 else (x.stride(0), x.stride(1)) for x in codes)
+    return Cache(c, cu_host, cu_dev, lengths, *codes, *scales)
+
+
+def dam_cache_sizes(cache: Cache, Hq: int):
+    """(rows of the scales, bytes of dam_cache_decode_attention's scratch)."""
+    rows, scratch = ctypes.c_size_t(0), ctypes.c_size_t(0)
+    _check(lib().dam_cache_sizes(cache.ref, Hq, ctypes.byref(rows), ctypes.byref(scratch)), "dam_cache_sizes")
+    return rows.value, scratch.value
+
+
+def _check_starts(starts: Optional[torch.Tensor], cache: Cache):
+    if starts is not None:
+        assert starts.dtype == torch.int32 and starts.numel() == cache.c.num_seqs and starts.is_contiguous()
+
+
+def dam_cache_write(K: torch.Tensor, V: torch.Tensor, tokens: Shape, cache: Cache, starts: Optional[torch.Tensor] = None,
+                    scratch: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Quantises the packed rows K, V (`tokens` says how many each sequence gets) into the cache, from token starts[b] of
+    sequence b on (int32 on the device; None: token 0).  Returns scratch."""
+    _check_starts(starts, cache)
+    if scratch is None:
+        scratch = _alloc(256, K.device)
+    rc = lib().dam_cache_write(_ptr(K), _ptr(V), tokens.ref, _ptr(starts), cache.ref, _ptr(scratch), scratch.numel(), _stream(K.device))
+    _check(rc, "dam_cache_write")
+    return scratch
+
+
+def dam_cache_read(cache: Cache, tokens: Shape, starts: Optional[torch.Tensor] = None, K: Optional[torch.Tensor] = None,
+                   V: Optional[torch.Tensor] = None, scratch: Optional[torch.Tensor] = None):
+    """Reads tokens starts[b] ... of every sequence back, as packed rows (`tokens` says how many, of which type and strides).
+    Returns (K, V, scratch)."""
+    _check_starts(starts, cache)
+    device = cache.k_codes.device
+    if K is None or V is None:
+        s = tokens.c
+        rows = [torch.empty_strided((s.total_tokens, s.num_kv_heads, s.head_dim), (*strides, 1), device=device,
+                                    dtype=torch.bfloat16 if s.dtype == DAM_BF16 else torch.float32)
+                for strides in ((s.k_stride_tok, s.k_stride_head), (s.v_stride_tok, s.v_stride_head))]
+        K, V = K if K is not None else rows[0], V if V is not None else rows[1]
+    if scratch is None:
+        scratch = _alloc(256, device)
+    rc = lib().dam_cache_read(cache.ref, tokens.ref, _ptr(starts), _ptr(K), _ptr(V), _ptr(scratch), scratch.numel(), _stream(device))
+    _check(rc, "dam_cache_read")
+    return K, V, scratch
+
+
+def dam_cache_decode_attention(q: torch.Tensor, cache: Cache, positions: torch.Tensor, mask: Optional[torch.Tensor] = None,
+                               softmax_scale: float = 0.0, O: Optional[torch.Tensor] = None,
+                               lse: Optional[torch.Tensor] = None, scratch: Optional[torch.Tensor] = None):
+    """One new token per sequence against an 8-bit cache (q, O: [B, Hq, d]; positions int32 [B]): every key up to its position,
+    or, with a mask blob, those that its patterns keep.  Returns (O, LSE [B, Hq] fp32, scratch)."""
+    B, Hq = cache.c.num_seqs, q.shape[1]
+    assert q.is_contiguous() and q.shape == (B, Hq, cache.c.head_dim)
+    assert positions.dtype == torch.int32 and positions.numel() == B and positions.is_contiguous()
+    if O is None:
+        O = torch.empty_like(q)
+    if lse is None:
+        lse = torch.empty(B, Hq, dtype=torch.float32, device=q.device)
+    if scratch is None:
+        scratch = _alloc(dam_cache_sizes(cache, Hq)[1], q.device)
+    rc = lib().dam_cache_decode_attention(_ptr(q), cache.ref, _ptr(mask), _ptr(positions), Hq,
+                                          DAM_BF16 if q.dtype == torch.bfloat16 else DAM_F32, softmax_scale, _ptr(O),
+                                          _ptr(lse), _ptr(scratch), scratch.numel(), _stream(q.device))
+    _check(rc, "dam_cache_decode_attention")
     return O, lse, scratch
 
 

@@ -6,6 +6,7 @@
 #include <mutex>
 #include <vector>
 
+#include "dam_cache.cuh"
 #include "dam_internal.cuh"
 
 namespace {
@@ -452,6 +453,86 @@ dam_status_t dam_decode_attention(const void* q, const void* K, const void* V, c
   cudaError_t e = dam_launch_decode(q, K, V, mask, shape, positions_dev, scale, O, lse, scratch, cs);
   if (e == cudaErrorNotSupported) return DAM_ERR_UNSUPPORTED;
   return e == cudaSuccess ? DAM_OK : DAM_ERR_CUDA;
+}
+
+namespace {
+
+dam_status_t check_cache(const dam_cache_t* c, bool buffers) {
+  if (!c || c->struct_size != sizeof(dam_cache_t) || c->reserved != 0) return DAM_ERR_INVALID_ARGUMENT;
+  if (c->num_seqs < 1 || !c->cu_seqlens_host || !c->cu_seqlens_dev || c->cu_seqlens_host[0] != 0) return DAM_ERR_INVALID_ARGUMENT;
+  for (int b = 0; b < c->num_seqs; ++b)
+    if (c->cu_seqlens_host[b + 1] < c->cu_seqlens_host[b]) return DAM_ERR_INVALID_ARGUMENT;
+  // (a position and the end of its block are 32-bit numbers in the kernels)
+  if (c->cu_seqlens_host[c->num_seqs] != c->total_tokens || c->total_tokens > 0x7FFFFFFF - 255) return DAM_ERR_INVALID_ARGUMENT;
+  if (c->num_kv_heads < 1 || (c->code != DAM_CODE_INT8 && c->code != DAM_CODE_E4M3)) return DAM_ERR_INVALID_ARGUMENT;
+  if (c->block_tokens != 16 && c->block_tokens != 32 && c->block_tokens != 64 && c->block_tokens != 128) return DAM_ERR_INVALID_ARGUMENT;
+  if (c->head_dim != 64 && c->head_dim != 128) return DAM_ERR_UNSUPPORTED;
+  const int64_t st[4] = {c->k_stride_tok, c->k_stride_head, c->v_stride_tok, c->v_stride_head};
+  for (int i = 0; i < 4; ++i)
+    if (st[i] < c->head_dim || st[i] % 16) return DAM_ERR_INVALID_ARGUMENT;
+  if (buffers && (!c->k_codes || !c->v_codes || !c->k_scales || !c->v_scales || !aligned(c->k_codes, 16) || !aligned(c->v_codes, 16) ||
+                  !aligned(c->k_scales, 4) || !aligned(c->v_scales, 4)))
+    return DAM_ERR_INVALID_ARGUMENT;
+  return DAM_OK;
+}
+
+// what a write and a read have in common
+dam_status_t check_cache_rows(const dam_cache_t* cache, const dam_shape_t* tokens, const int32_t* starts_dev, const void* K, const void* V,
+                              const void* scratch, size_t scratch_bytes) {
+  dam_status_t st;
+  if ((st = check_shape(tokens)) != DAM_OK) return st;
+  if ((st = check_cache(cache, true)) != DAM_OK) return st;
+  if (tokens->num_seqs != cache->num_seqs || tokens->num_kv_heads != cache->num_kv_heads || tokens->head_dim != cache->head_dim)
+    return DAM_ERR_INVALID_ARGUMENT;
+  if (!K || !V || !scratch || !aligned(K, 16) || !aligned(V, 16) || !aligned(scratch, 256) || (starts_dev && !aligned(starts_dev, 4)))
+    return DAM_ERR_INVALID_ARGUMENT;
+  if (tokens->total_tokens > 0x7FFFFFFF - 255) return DAM_ERR_INVALID_ARGUMENT;
+  return scratch_bytes < 256 ? DAM_ERR_BUFFER_TOO_SMALL : DAM_OK;
+}
+
+dam_status_t launched(cudaError_t e) {
+  return e == cudaSuccess ? DAM_OK : e == cudaErrorNotSupported ? DAM_ERR_UNSUPPORTED : DAM_ERR_CUDA;
+}
+
+}  // namespace
+
+dam_status_t dam_cache_sizes(const dam_cache_t* cache, int32_t num_q_heads, size_t* scale_rows, size_t* scratch_bytes) {
+  dam_status_t st;
+  if ((st = check_cache(cache, false)) != DAM_OK) return st;
+  if (num_q_heads < 1 || num_q_heads % cache->num_kv_heads) return DAM_ERR_INVALID_ARGUMENT;
+  if (scale_rows) *scale_rows = (size_t)(cache->total_tokens / cache->block_tokens) + (size_t)cache->num_seqs;
+  if (scratch_bytes) *scratch_bytes = dam_cache_scratch_bytes(cache->head_dim);
+  return DAM_OK;
+}
+
+dam_status_t dam_cache_write(const void* K, const void* V, const dam_shape_t* tokens, const int32_t* starts_dev,
+                             const dam_cache_t* cache, void* scratch, size_t scratch_bytes, void* stream) {
+  const dam_status_t st = check_cache_rows(cache, tokens, starts_dev, K, V, scratch, scratch_bytes);
+  if (st != DAM_OK) return st;
+  return launched(dam_launch_cache_write(K, V, tokens, starts_dev, cache, scratch, reinterpret_cast<cudaStream_t>(stream)));
+}
+
+dam_status_t dam_cache_read(const dam_cache_t* cache, const dam_shape_t* tokens, const int32_t* starts_dev, void* K, void* V,
+                            void* scratch, size_t scratch_bytes, void* stream) {
+  const dam_status_t st = check_cache_rows(cache, tokens, starts_dev, K, V, scratch, scratch_bytes);
+  if (st != DAM_OK) return st;
+  return launched(dam_launch_cache_read(cache, tokens, starts_dev, K, V, scratch, reinterpret_cast<cudaStream_t>(stream)));
+}
+
+dam_status_t dam_cache_decode_attention(const void* q, const dam_cache_t* cache, const void* mask, const int32_t* positions_dev,
+                                        int32_t num_q_heads, int32_t dtype, float softmax_scale, void* O, float* lse,
+                                        void* scratch, size_t scratch_bytes, void* stream) {
+  dam_status_t st;
+  if ((st = check_cache(cache, true)) != DAM_OK) return st;
+  if (!q || !positions_dev || !O || !lse || !scratch || !aligned(q, 16) || !aligned(O, 16) || !aligned(lse, 4) ||
+      !aligned(positions_dev, 4) || !aligned(mask, 256) || !aligned(scratch, 256))
+    return DAM_ERR_INVALID_ARGUMENT;
+  if (num_q_heads < 1 || num_q_heads % cache->num_kv_heads || !(softmax_scale >= 0.f) || (dtype != DAM_BF16 && dtype != DAM_F32))
+    return DAM_ERR_INVALID_ARGUMENT;
+  if (scratch_bytes < dam_cache_scratch_bytes(cache->head_dim)) return DAM_ERR_BUFFER_TOO_SMALL;
+  const float scale = softmax_scale > 0.f ? softmax_scale : 1.0f / sqrtf((float)cache->head_dim);
+  return launched(dam_launch_cache_decode(q, cache, mask, positions_dev, num_q_heads, dtype, scale, O, lse, scratch,
+                                          reinterpret_cast<cudaStream_t>(stream)));
 }
 
 dam_status_t dam_mask_stats(const void* mask, const dam_shape_t* shape, uint64_t* out, uint64_t* active_elems_dev,

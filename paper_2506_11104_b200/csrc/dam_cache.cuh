@@ -1,0 +1,137 @@
+// The KV cache held in 8 bits: how the kernels see it, and the arithmetic of its codes and scales (dam.h states the rule).
+#pragma once
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+#include "dam_internal.cuh"
+
+// dam_cache_t as the kernels take it, by value.  The scales of block j of sequence b stand in row cu[b] / block + b + j.
+struct DamCacheView {
+  const int32_t* cu;
+  int32_t num_seqs, Hkv;
+  int32_t shift;                 // log2 of block_tokens
+  unsigned char *k, *v;
+  float *ks, *vs;
+  int64_t kst, ksh, vst, vsh;    // bytes
+};
+
+inline DamCacheView dam_cache_view(const dam_cache_t* c) {
+  DamCacheView v;
+  v.cu = c->cu_seqlens_dev; v.num_seqs = c->num_seqs; v.Hkv = c->num_kv_heads;
+  v.shift = 0;
+  while ((1 << v.shift) < c->block_tokens) ++v.shift;
+  v.k = reinterpret_cast<unsigned char*>(c->k_codes); v.v = reinterpret_cast<unsigned char*>(c->v_codes);
+  v.ks = c->k_scales; v.vs = c->v_scales;
+  v.kst = c->k_stride_tok; v.ksh = c->k_stride_head; v.vst = c->v_stride_tok; v.vsh = c->v_stride_head;
+  return v;
+}
+
+// ---- codes -> values ----------------------------------------------------------------------------
+// Two e4m3 codes (low byte first) as two fp16 numbers: exact, fp16 has more exponent and mantissa bits.
+__device__ __forceinline__ uint32_t e4m3x2_to_half2(uint32_t codes16) {
+  uint32_t h;
+  asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"((unsigned short)codes16));
+  return h;
+}
+// Two int8 codes that were XORed with 0x80 (so they read c + 128) and placed under the byte 0x64, i.e. the fp16 numbers
+// 1024 + 128 + c, whose spacing is 1: minus 1152 is c, exactly.
+__device__ __forceinline__ uint32_t biased_to_half2(uint32_t h) {
+  uint32_t r;
+  asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(h), "r"(0x64806480u));
+  return r;
+}
+// The four codes of a word as fp32 numbers.
+template <int CODE>
+__device__ __forceinline__ void codes_to_float(uint32_t w, float* f) {
+  if constexpr (CODE == DAM_CODE_INT8) {
+    // 2^23 + 128 + c as fp32 bits, minus 2^23 + 128
+    w ^= 0x80808080u;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) f[k] = __uint_as_float(__byte_perm(w, 0x4B000000u, 0x7440 | k)) - 8388736.f;
+  } else {
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      const uint32_t h = e4m3x2_to_half2(w >> (16 * k));
+      const float2 v = __half22float2(*reinterpret_cast<const __half2*>(&h));
+      f[2 * k] = v.x; f[2 * k + 1] = v.y;
+    }
+  }
+}
+
+// ---- values -> codes ----------------------------------------------------------------------------
+__device__ __forceinline__ float dam_cache_nan() { return __uint_as_float(0x7FC00000u); }
+
+// The scale of a block whose largest magnitude has the bits `amax` (sign bit clear).  A block with an infinity or a NaN has
+// none: its scale is a NaN, and so is every value read back from it.
+template <int CODE>
+__device__ __forceinline__ float cache_scale(uint32_t amax) {
+  if (amax >= 0x7F800000u) return dam_cache_nan();
+  if constexpr (CODE == DAM_CODE_INT8) {
+    return fmaxf(__fdiv_rn(__uint_as_float(amax), 127.f), 1.17549435e-38f);
+  } else {
+    // amax = M 2^E: the least k with M 2^E <= 1.75 * 2^8 * 2^k is E - 8, plus 1 when M > 1.75 (mantissa bits above 0x600000)
+    const int e = (int)((amax + 0x1FFFFFu) >> 23) - 8;
+    return __uint_as_float((uint32_t)(e < 1 ? 1 : e) << 23);
+  }
+}
+
+// The code of x under the scale s (inv = 1 / s), as the low byte.
+template <int CODE>
+__device__ __forceinline__ uint32_t cache_code(float x, float s, float inv) {
+  if constexpr (CODE == DAM_CODE_INT8) {
+    // nearest integer to x / s, ties to even, decided on the exact quotient: x * inv is off by 127 * 2^-23 at most, so q is
+    // right or, next to a border, one off; x - q s is exact there (a multiple of half an ulp of s, at most s / 2 (1 + 2^-15))
+    float q = rintf(x * inv);
+    const float r = fmaf(-q, s, x), half = 0.5f * s;
+    if (fabsf(r) >= half) {
+      const bool odd = ((int)q & 1) != 0;
+      if (r > half || (r == half && odd)) q += 1.f;
+      else if (r < -half || (r == -half && odd)) q -= 1.f;
+    }
+    const int c = max(-127, min(127, (int)q));
+    return (uint32_t)c & 0xFFu;
+  } else {
+    // (the scale is a power of two: x * inv is exact, or so small that its code is zero)
+    uint16_t p;
+    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(p) : "f"(0.f), "f"(x * inv));
+    return p & 0xFFu;
+  }
+}
+
+// ---- which sequence -----------------------------------------------------------------------------
+// The work of a packed batch is cut into slots: sequence b owns the slots (cu[b] >> shift) + extra * b onwards, up to the next
+// sequence's.  Returns the sequence of a slot (whole warp; a step looks at 32 places at once).
+__device__ __forceinline__ int cache_seq_of_slot(const int32_t* __restrict__ cu, int n, int shift, int extra, int64_t slot) {
+  int lo = 0, hi = n;
+  const int lane = threadIdx.x & 31;
+  while (hi - lo > 1) {
+    const int step = (hi - lo + 31) >> 5, b = lo + lane * step;
+    const bool here = b < hi && (int64_t)(__ldg(cu + b) >> shift) + (int64_t)extra * b <= slot;
+    const int cnt = __popc(__ballot_sync(0xFFFFFFFFu, here));
+    lo += (cnt - 1) * step;
+    hi = min(hi, lo + step);
+  }
+  return lo;
+}
+
+// ---- host: dispatch ----------------------------------------------------------------------------
+// FN<T, D, CODE>(...) for the types at hand
+#define DAM_CACHE_DISPATCH(FN, dtype, dim, code, ...)                                                                          \
+  (dtype == DAM_BF16 ? (dim == 128 ? (code == DAM_CODE_INT8 ? FN<__nv_bfloat16, 128, DAM_CODE_INT8>(__VA_ARGS__)               \
+                                                            : FN<__nv_bfloat16, 128, DAM_CODE_E4M3>(__VA_ARGS__))              \
+                                   : (code == DAM_CODE_INT8 ? FN<__nv_bfloat16, 64, DAM_CODE_INT8>(__VA_ARGS__)                \
+                                                            : FN<__nv_bfloat16, 64, DAM_CODE_E4M3>(__VA_ARGS__)))              \
+                     : (dim == 128 ? (code == DAM_CODE_INT8 ? FN<float, 128, DAM_CODE_INT8>(__VA_ARGS__)                       \
+                                                            : FN<float, 128, DAM_CODE_E4M3>(__VA_ARGS__))                      \
+                                   : (code == DAM_CODE_INT8 ? FN<float, 64, DAM_CODE_INT8>(__VA_ARGS__)                        \
+                                                            : FN<float, 64, DAM_CODE_E4M3>(__VA_ARGS__))))
+
+// ---- launch entry points ------------------------------------------------------------------------
+cudaError_t dam_launch_cache_write(const void* K, const void* V, const dam_shape_t* tokens, const int32_t* starts, const dam_cache_t* cache,
+                                   void* scratch, cudaStream_t st);
+cudaError_t dam_launch_cache_read(const dam_cache_t* cache, const dam_shape_t* tokens, const int32_t* starts, void* K, void* V,
+                                  void* scratch, cudaStream_t st);
+// bytes of scratch that the attention over a cache wants (partial results of sequences that several blocks share)
+size_t dam_cache_scratch_bytes(int head_dim);
+cudaError_t dam_launch_cache_decode(const void* q, const dam_cache_t* cache, const void* mask, const int32_t* positions, int Hq, int dtype,
+                                    float scale, void* O, float* lse, void* scratch, cudaStream_t st);

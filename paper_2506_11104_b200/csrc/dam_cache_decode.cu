@@ -1,0 +1,817 @@
+// Generation over a KV cache held in 8 bits: one new token per sequence, against every key its sequence holds, or against the
+// keys that the patterns of a mask blob keep (paper Sec. 4.3, Case 2).
+//
+// The logit of key j is scale * sK(j) * (q . codes of K_j), the output sum_j p_j sV(j) (codes of V_j) / sum_j p_j: the codes go
+// through the warp-level tensor-core instruction as fp16 numbers, which hold every int8 and every e4m3 value exactly, and the
+// scales are applied to the logits and to the probabilities, one multiplication per key and head instead of one per element.
+// Both products are taken transposed, S^T = K q^T and O^T = V^T P^T: the 8 query heads of a KV head are the narrow side of the
+// instruction's tile, so nothing of it is padding where a group has 8 heads.  fp16 operands: q is scaled by a power of two so
+// that its largest element lies in [2^14, 2^15) (a bf16 q is then exact wherever it matters), the probabilities are taken
+// relative to a running maximum times sV over a running reference, at most 2^15.  An fp32 q and its probabilities are each the
+// sum of two fp16 numbers (22 bits), at the price of twice the instructions.
+//
+// A warp works on slices of 16 keys, brought to shared memory by asynchronous copies some slices ahead, and keeps a running
+// softmax and its share of O^T of its own; the warps of a block meet at the end of a sequence's share only.  The order of the
+// dimensions inside the instructions' k side and of O^T's rows is free, and taken so that every lane reads its codes 16 bytes
+// at a time and, with K, a register of four codes is two operand registers.
+//
+// Bound by HBM: 2 d bytes and two scales per key and KV head are read once.
+#include <cooperative_groups.h>
+#include <math_constants.h>
+
+#include "dam_cache.cuh"
+#include "dam_decode_common.cuh"
+
+namespace {
+
+constexpr int kSlice = 16;             // keys of a slice: the rows of the first instruction, the k side of the second
+
+__device__ __forceinline__ void cp_async16_zfill(uint32_t dst, const void* src, uint32_t bytes) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void cp_async4_zfill(uint32_t dst, const void* src, uint32_t bytes) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ uint4 lds128(uint32_t a) {
+  uint4 r;
+  asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(r.x), "=r"(r.y), "=r"(r.z), "=r"(r.w) : "r"(a));
+  return r;
+}
+__device__ __forceinline__ uint2 lds64(uint32_t a) {
+  uint2 r;
+  asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(r.x), "=r"(r.y) : "r"(a));
+  return r;
+}
+__device__ __forceinline__ float lds_float(uint32_t a) {
+  float r;
+  asm volatile("ld.shared.f32 %0, [%1];" : "=f"(r) : "r"(a));
+  return r;
+}
+// D (16 x 8, fp32) += A (16 x 16, fp16, row-major) * B (16 x 8, fp16, column-major)
+__device__ __forceinline__ void mma_f16(float* c, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+               : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t pack_half2(float lo, float hi) {
+  const __half2 h = __floats2half2_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+// four codes in memory order -> two operand registers (codes 0, 1 and codes 2, 3)
+template <int CODE>
+__device__ __forceinline__ void codes_to_half(uint32_t w, uint32_t* h) {
+  if constexpr (CODE == DAM_CODE_INT8) {
+    w ^= 0x80808080u;
+    h[0] = biased_to_half2(__byte_perm(w, 0x64646464u, 0x4140));
+    h[1] = biased_to_half2(__byte_perm(w, 0x64646464u, 0x4342));
+  } else {
+    h[0] = e4m3x2_to_half2(w & 0xFFFFu);
+    h[1] = e4m3x2_to_half2(w >> 16);
+  }
+}
+
+// Shared memory of one slice: 16 K rows, 16 V rows, 16 K scales, 16 V scales.  The 16-byte pieces of the rows are permuted so
+// that the eight lanes a 16-byte read is served for at a time find their pieces in different banks:
+//   head_dim 128: piece p of row r stands at p ^ (r & 7);
+//   head_dim 64:  two rows share 128 bytes; piece p of row r stands at ((r & 1) * 4 + p) ^ 2 * (r / 2 & 3) of them.
+template <int D>
+struct Slice {
+  static constexpr int pieces = D / 16;
+  static constexpr int v_off = kSlice * D, scale_off = 2 * kSlice * D, bytes = 2 * kSlice * D + 2 * kSlice * 4;
+  static __device__ __forceinline__ uint32_t at(int r, int p) {
+    if constexpr (D == 128) return r * 128 + ((p ^ (r & 7)) << 4);
+    else return (r >> 1) * 128 + ((((r & 1) * 4 + p) ^ ((r >> 1 & 3) * 2)) << 4);
+  }
+};
+
+// What a warp carries through the keys of one (sequence, up to 8 query heads of one KV head).  Lane = 4 row + quad: the lane
+// holds the logits of keys row and row + 8 against heads 2 quad and 2 quad + 1, and of O^T the dimensions D / 8 * row ... of the
+// same two heads.
+template <typename T, int D, int CODE>
+struct WarpState {
+  static constexpr bool kSplit = sizeof(T) == 4;             // q and P as two fp16 numbers each
+  static constexpr int KS = D / 16;
+  uint32_t qh[KS][2], ql[kSplit ? KS : 1][2];
+  float qs[2];                         // logits (log2 units) per product of codes and q as it is held, of the lane's heads
+  float m[2], l[2];                    // reference (log2 units) and the lane's share of the sum
+  float vinv;                          // the reference of the V scales: P is held times sV * vinv
+  float o[KS][4];                      // [u][0..1]: dimension D / 8 * row + 2 u, the lane's heads; [u][2..3]: the next dimension
+
+  __device__ __forceinline__ void reset() {
+    m[0] = m[1] = -CUDART_INF_F;
+    l[0] = l[1] = 0.f;
+    vinv = 1.6225927682921336e32f;     // 2^107
+#pragma unroll
+    for (int u = 0; u < KS; ++u) o[u][0] = o[u][1] = o[u][2] = o[u][3] = 0.f;
+  }
+
+  // q: row of the first head; `heads` of them exist
+  __device__ __forceinline__ void load_q(const T* q, int heads, float scale_log2) {
+    const int lane = threadIdx.x & 31, row = lane >> 2, quad = lane & 3;
+    constexpr int N = D / 4;                                 // the lane's elements of head `row`: dimensions N quad ...
+    float x[N];
+    const T* p = q + (int64_t)(row < heads ? row : 0) * D + N * quad;
+    if constexpr (kSplit) {
+#pragma unroll
+      for (int i = 0; i < N / 4; ++i) {
+        const float4 a = __ldg(reinterpret_cast<const float4*>(p) + i);
+        x[4 * i] = a.x; x[4 * i + 1] = a.y; x[4 * i + 2] = a.z; x[4 * i + 3] = a.w;
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < N / 8; ++i) {
+        const uint4 a = __ldg(reinterpret_cast<const uint4*>(p) + i);
+        const uint32_t w[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+        for (int k = 0; k < 4; ++k) { x[8 * i + 2 * k] = __uint_as_float(w[k] << 16); x[8 * i + 2 * k + 1] = __uint_as_float(w[k] & 0xFFFF0000u); }
+      }
+    }
+    uint32_t top = 0u;
+#pragma unroll
+    for (int i = 0; i < N; ++i) top = max(top, __float_as_uint(x[i]) & 0x7FFFFFFFu);
+    top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
+    top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
+    // 2^(14 - exponent of the largest); an infinity or a NaN stays one
+    const int f = min(268 - (int)(top >> 23), 253);
+    const float mul = row < heads ? __uint_as_float((uint32_t)f << 23) : 0.f;
+#pragma unroll
+    for (int s = 0; s < KS; ++s) {
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        const float a = x[4 * s + 2 * k] * mul, b = x[4 * s + 2 * k + 1] * mul;
+        qh[s][k] = pack_half2(a, b);
+        if constexpr (kSplit) {
+          const float2 hi = __half22float2(*reinterpret_cast<const __half2*>(&qh[s][k]));
+          ql[s][k] = pack_half2(a - hi.x, b - hi.y);
+        }
+      }
+    }
+    const float back = scale_log2 * __uint_as_float((uint32_t)(254 - f) << 23);
+    qs[0] = __shfl_sync(0xFFFFFFFFu, back, 8 * quad);
+    qs[1] = __shfl_sync(0xFFFFFFFFu, back, 8 * quad + 4);
+  }
+
+  // One slice.  keep: bit e (e + 2): head 2 quad + e keeps key row (row + 8); a key that a head does not keep has no part in it.
+  __device__ __forceinline__ void step(uint32_t slice, uint32_t keep) {
+    using SL = Slice<D>;
+    const int lane = threadIdx.x & 31, row = lane >> 2, quad = lane & 3;
+    const float ks0 = lds_float(slice + SL::scale_off + 4 * row), ks1 = lds_float(slice + SL::scale_off + 4 * row + 32);
+    const float vs0 = lds_float(slice + SL::scale_off + 64 + 4 * row), vs1 = lds_float(slice + SL::scale_off + 96 + 4 * row);
+    // S^T = K q^T: k-step s takes the dimensions D / 4 * quad + 4 s ... of a lane
+    float st[2][4] = {};                                     // (two chains of instructions, half as long)
+#pragma unroll
+    for (int c = 0; c < D / 64; ++c) {
+      const uint4 a = lds128(slice + SL::at(row, D / 64 * quad + c)), b = lds128(slice + SL::at(row + 8, D / 64 * quad + c));
+      const uint32_t wa[4] = {a.x, a.y, a.z, a.w}, wb[4] = {b.x, b.y, b.z, b.w};
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int s = 4 * c + i;
+        uint32_t ha[2], hb[2];
+        codes_to_half<CODE>(wa[i], ha);
+        codes_to_half<CODE>(wb[i], hb);
+        mma_f16(st[s & 1], ha[0], hb[0], ha[1], hb[1], qh[s][0], qh[s][1]);
+        if constexpr (kSplit) mma_f16(st[s & 1], ha[0], hb[0], ha[1], hb[1], ql[s][0], ql[s][1]);
+      }
+    }
+    float x[4];
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      x[e] = keep >> e & 1u ? (st[0][e] + st[1][e]) * (ks0 * qs[e]) : -CUDART_INF_F;
+      x[2 + e] = keep >> (2 + e) & 1u ? (st[0][2 + e] + st[1][2 + e]) * (ks1 * qs[e]) : -CUDART_INF_F;
+    }
+    // the reference moves when a logit lies more than 8 above it: probabilities stay below 2^8, and most slices move nothing
+    const bool up = fmaxf(x[0], x[2]) > m[0] + 8.f || fmaxf(x[1], x[3]) > m[1] + 8.f;
+    if (__any_sync(0xFFFFFFFFu, up)) {
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        float mx = fmaxf(x[e], x[2 + e]);
+        mx = fmaxf(mx, __shfl_xor_sync(0xFFFFFFFFu, mx, 4));
+        mx = fmaxf(mx, __shfl_xor_sync(0xFFFFFFFFu, mx, 8));
+        mx = fmaxf(mx, __shfl_xor_sync(0xFFFFFFFFu, mx, 16));
+        const float mn = fmaxf(m[e], mx);
+        const float alpha = mn == -CUDART_INF_F ? 1.f : g_ex2(m[e] - mn);
+        m[e] = mn;
+        l[e] *= alpha;
+#pragma unroll
+        for (int u = 0; u < KS; ++u) { o[u][e] *= alpha; o[u][2 + e] *= alpha; }
+      }
+    }
+    // and the reference of the V scales when one of them reaches 128 times it
+    if (__any_sync(0xFFFFFFFFu, (keep & 3u && vs0 * vinv > 128.f) || (keep & 12u && vs1 * vinv > 128.f))) {
+      float top = fmaxf(keep & 3u ? vs0 : 0.f, keep & 12u ? vs1 : 0.f);
+#pragma unroll
+      for (int d = 1; d < 32; d <<= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, d));
+      const int f = max(1, min(234, 260 - (int)(__float_as_uint(top) >> 23)));     // top * 2^(f - 127) lies in [64, 128)
+      const float now = __uint_as_float((uint32_t)f << 23), ratio = now / vinv;
+      vinv = now;
+#pragma unroll
+      for (int u = 0; u < KS; ++u) { o[u][0] *= ratio; o[u][1] *= ratio; o[u][2] *= ratio; o[u][3] *= ratio; }
+    }
+    float w[4];
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      const float ref = m[e] == -CUDART_INF_F ? 0.f : m[e];  // (no key yet, or logits of -inf alone: no weight)
+      const float p0 = g_ex2(x[e] - ref), p1 = g_ex2(x[2 + e] - ref);
+      l[e] += p0 + p1;
+      // (a key that is not kept may stand in a block without a scale: 0 * NaN is not 0)
+      w[e] = keep >> e & 1u ? p0 * (vs0 * vinv) : 0.f;
+      w[2 + e] = keep >> (2 + e) & 1u ? p1 * (vs1 * vinv) : 0.f;
+    }
+    // P^T as operands (k = key, n = head): the transposes of the two 8 x 8 blocks [key][head]
+    const uint32_t h0 = pack_half2(w[0], w[1]), h1 = pack_half2(w[2], w[3]);
+    const uint32_t pb0 = movmatrix_trans(h0), pb1 = movmatrix_trans(h1);
+    uint32_t pl0 = 0u, pl1 = 0u;
+    if constexpr (kSplit) {
+      const float2 f0 = __half22float2(*reinterpret_cast<const __half2*>(&h0)), f1 = __half22float2(*reinterpret_cast<const __half2*>(&h1));
+      pl0 = movmatrix_trans(pack_half2(w[0] - f0.x, w[1] - f0.y));
+      pl1 = movmatrix_trans(pack_half2(w[2] - f1.x, w[3] - f1.y));
+    }
+    // O^T += V^T P^T: the lane's rows are keys 2 quad, 2 quad + 1, 2 quad + 8, 2 quad + 9; their codes of one dimension are
+    // brought together byte by byte
+    uint32_t vw[4][D / 32];
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const int key = 2 * quad + (r & 1) + (r >> 1) * 8;
+      if constexpr (D == 128) {
+        const uint4 a = lds128(slice + SL::v_off + SL::at(key, row));
+        vw[r][0] = a.x; vw[r][1] = a.y; vw[r][2] = a.z; vw[r][3] = a.w;
+      } else {
+        const uint2 a = lds64(slice + SL::v_off + SL::at(key, row >> 1) + (row & 1) * 8);
+        vw[r][0] = a.x; vw[r][1] = a.y;
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i) {
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        // (bytes 2 k, 2 k + 1 of either key: dimension 4 i + 2 k of both keys, then dimension 4 i + 2 k + 1)
+        const uint32_t sel = k ? 0x7362u : 0x5140u;
+        uint32_t a[2], b[2];
+        codes_to_half<CODE>(__byte_perm(vw[0][i], vw[1][i], sel), a);
+        codes_to_half<CODE>(__byte_perm(vw[2][i], vw[3][i], sel), b);
+        const int u = 2 * i + k;
+        mma_f16(o[u], a[0], a[1], b[0], b[1], pb0, pb1);
+        if constexpr (kSplit) mma_f16(o[u], a[0], a[1], b[0], b[1], pl0, pl1);
+      }
+    }
+  }
+
+  // The warp's state to shared memory: [head][kRow] floats, O at position 16 u + 2 row + (0, 1) for dimension D / 8 * row + 2 u +
+  // (0, 1), then the reference and the sum.  (kRow: the lanes of a store fall into different banks.)
+  static constexpr int kRow = D + 4;
+  __device__ __forceinline__ void store(float* mg) {
+    const int lane = threadIdx.x & 31, row = lane >> 2, quad = lane & 3;
+    const float back = 1.f / vinv;
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      float s = l[e];
+      s += __shfl_xor_sync(0xFFFFFFFFu, s, 4);
+      s += __shfl_xor_sync(0xFFFFFFFFu, s, 8);
+      s += __shfl_xor_sync(0xFFFFFFFFu, s, 16);
+      float* dst = mg + (2 * quad + e) * kRow;
+#pragma unroll
+      for (int u = 0; u < KS; ++u) *reinterpret_cast<float2*>(dst + 16 * u + 2 * row) = make_float2(o[u][e] * back, o[u][2 + e] * back);
+      if (row == 0) { dst[D] = m[e]; dst[D + 1] = s; }
+    }
+  }
+  // dimension that stands at position p of a stored row
+  static __device__ __forceinline__ int dim_at(int p) { return D / 8 * ((p & 15) >> 1) + 2 * (p >> 4) + (p & 1); }
+};
+
+__device__ __forceinline__ void put(float* p, float v) { *p = v; }
+__device__ __forceinline__ void put(__nv_bfloat16* p, float v) { *p = __float2bfloat16_rn(v); }
+__device__ __forceinline__ float lse_of(float m, float l) { return l == 0.f ? -CUDART_INF_F : (m + log2f(l)) * 0.6931471805599453f; }
+// weight of a partial result with reference m under the common reference mx (a partial result without a key has none)
+__device__ __forceinline__ float weight(float m, float mx) { return m == -CUDART_INF_F ? 0.f : g_ex2(m - mx); }
+
+struct CacheDecode {
+  const void* q;
+  const int32_t* pos;
+  int Hq, G, NS;               // query heads, per KV head, and groups of 8 of them per KV head
+  float scale_log2;
+  void* O;
+  float* lse;
+  uint32_t* scratch;
+};
+
+// ---- every key ----------------------------------------------------------------------------------
+// The keys of all (sequence, KV head, group of 8 heads) form one list of chunks (WARPS slices: one per warp), in that order; block
+// c of G takes the chunks [total c / G, total (c + 1) / G): every SM reads the same number of bytes, however ragged the batch.
+// Where a block's share ends inside a sequence's keys it leaves a partial result, and a second kernel joins those.
+constexpr int kMaxShares = 148;        // blocks: one per SM of a B200
+
+__device__ __forceinline__ int chunks_of(const DamCacheView& c, const int32_t* pos, int b, int chunk) {
+  const int p = __ldg(pos + b);
+  return p < 0 || p >= __ldg(c.cu + b + 1) - __ldg(c.cu + b) ? 0 : p / chunk + 1;
+}
+
+// Chunks per head over all sequences (whole warp).
+__device__ __forceinline__ int64_t total_chunks(const DamCacheView& c, const int32_t* pos, int chunk) {
+  int64_t sum = 0;
+  for (int b = threadIdx.x & 31; b < c.num_seqs; b += 32) sum += chunks_of(c, pos, b, chunk);
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
+  return sum;
+}
+
+// A place in the list of chunks.
+struct Place {
+  int b, len, n;               // sequence, its keys, its chunks per head
+  int hg, k;                   // KV head and group, chunk
+  int64_t row0;                // scale row of the sequence's first block
+  int64_t tok0;
+  __device__ __forceinline__ void enter(const DamCacheView& c, const int32_t* pos, int b_, int chunk) {
+    b = b_;
+    len = __ldg(pos + b) + 1;
+    n = chunks_of(c, pos, b, chunk);
+    tok0 = __ldg(c.cu + b);
+    row0 = (tok0 >> c.shift) + b;
+  }
+  // chunk `at` of the whole list (which has it)
+  __device__ __forceinline__ void locate(const DamCacheView& c, const int32_t* pos, int chunk, int heads, int64_t at) {
+    const int lane = threadIdx.x & 31;
+    int64_t before = 0;
+    for (int base = 0; base < c.num_seqs; base += 32) {
+      const int mine = base + lane < c.num_seqs ? chunks_of(c, pos, base + lane, chunk) : 0;
+      int64_t incl = mine;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const int64_t y = __shfl_up_sync(0xFFFFFFFFu, incl, o);
+        if (lane >= o) incl += y;
+      }
+      const uint32_t past = __ballot_sync(0xFFFFFFFFu, (before + incl) * heads > at);
+      if (past) {
+        const int w = __ffs(past) - 1;
+        const int64_t first = (before + __shfl_sync(0xFFFFFFFFu, incl - mine, w)) * heads;
+        enter(c, pos, base + w, chunk);
+        hg = (int)((at - first) / n);
+        k = (int)((at - first) % n);
+        return;
+      }
+      before += __shfl_sync(0xFFFFFFFFu, incl, 31);
+    }
+    b = len = n = hg = k = 0; row0 = tok0 = 0;
+  }
+  // the next chunk (there is one)
+  __device__ __forceinline__ void next(const DamCacheView& c, const int32_t* pos, int chunk, int heads) {
+    if (++k < n) return;
+    k = 0;
+    if (++hg < heads) return;
+    hg = 0;
+    do { enter(c, pos, b + 1, chunk); } while (n == 0 && b + 1 < c.num_seqs);
+  }
+};
+
+template <int D, int WARPS, int STAGES>
+struct DenseLayout {
+  static constexpr int chunk = WARPS * kSlice;
+  static constexpr int ring = WARPS * STAGES * Slice<D>::bytes;
+  static constexpr int total = ring + WARPS * kGMaxGroup * (D + 4) * 4;
+};
+// floats of one partial result: O of 8 heads, references, sums
+template <int D> constexpr int kPartial = kGMaxGroup * (D + 2);
+
+__device__ __forceinline__ int64_t share_begin(int64_t total, int c, int shares) { return total * c / shares; }
+
+template <typename T, int D, int CODE, int WARPS, int STAGES>
+__global__ void __launch_bounds__(WARPS * 32, 1)
+cache_decode_kernel(CacheDecode a, DamCacheView c, float* __restrict__ partial) {
+  dam_chain_prologue();
+  using LY = DenseLayout<D, WARPS, STAGES>;
+  using WS = WarpState<T, D, CODE>;
+  extern __shared__ __align__(128) unsigned char sm[];
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, shares = gridDim.x, heads = c.Hkv * a.NS;
+  float* mg = reinterpret_cast<float*>(sm + LY::ring);
+  const uint32_t ring = static_cast<uint32_t>(__cvta_generic_to_shared(sm)) + warp * (STAGES * Slice<D>::bytes);
+  // sequences whose position lies outside their capacity get zeros; block 0 says so in the status word
+  bool any = false;
+  for (int b = tid; b < c.num_seqs; b += WARPS * 32) any |= chunks_of(c, a.pos, b, LY::chunk) == 0;
+  any = __syncthreads_or(any);
+  if (blockIdx.x == 0 && tid < 64) a.scratch[tid] = tid == 1 && any ? (uint32_t)DAM_ERR_INVALID_ARGUMENT : 0u;
+  if (any) {
+    for (int b = blockIdx.x; b < c.num_seqs; b += shares) {
+      if (chunks_of(c, a.pos, b, LY::chunk)) continue;
+      for (int t = tid; t < a.Hq * D; t += WARPS * 32) put(reinterpret_cast<T*>(a.O) + (int64_t)b * a.Hq * D + t, 0.f);
+      for (int t = tid; t < a.Hq; t += WARPS * 32) a.lse[(int64_t)b * a.Hq + t] = -CUDART_INF_F;
+    }
+  }
+  const int64_t total = total_chunks(c, a.pos, LY::chunk) * heads;
+  const int64_t lo = share_begin(total, blockIdx.x, shares), hi = share_begin(total, blockIdx.x + 1, shares);
+  if (lo == hi) return;
+  Place in, cur;
+  in.locate(c, a.pos, LY::chunk, heads, lo);
+  cur = in;
+
+  auto issue = [&](const Place& p, int stage) {
+    const int key0 = p.k * LY::chunk + warp * kSlice;
+    if (key0 < p.len) {
+      const int kvh = p.hg / a.NS;
+      const uint32_t dst = ring + stage * Slice<D>::bytes;
+      const unsigned char* K = c.k + (p.tok0 + key0) * c.kst + (int64_t)kvh * c.ksh;
+      const unsigned char* V = c.v + (p.tok0 + key0) * c.vst + (int64_t)kvh * c.vsh;
+      const int live = p.len - key0;                         // keys of the slice that exist; the others are filled with zeros
+#pragma unroll
+      for (int i = 0; i < kSlice * Slice<D>::pieces / 32; ++i) {
+        const int x = lane + 32 * i, r = x / Slice<D>::pieces, piece = x % Slice<D>::pieces;
+        const int from = r < live ? r : 0;
+        const uint32_t n = r < live ? 16u : 0u, at = Slice<D>::at(r, piece);
+        cp_async16_zfill(dst + at, K + from * c.kst + piece * 16, n);
+        cp_async16_zfill(dst + Slice<D>::v_off + at, V + from * c.vst + piece * 16, n);
+      }
+      const int r = lane & 15, from = r < live ? r : 0;
+      const float* s = (lane < 16 ? c.ks : c.vs) + (p.row0 + ((key0 + from) >> c.shift)) * c.Hkv + kvh;
+      cp_async4_zfill(dst + Slice<D>::scale_off + 4 * lane, s, r < live ? 4u : 0u);
+    }
+  };
+  // (a group is committed every time, so that "all but the newest STAGES - 1" always includes this chunk's)
+#pragma unroll
+  for (int s = 0; s < STAGES - 1; ++s) {
+    if (lo + s < hi) {
+      if (s) in.next(c, a.pos, LY::chunk, heads);
+      issue(in, s);
+    }
+    cp_async_commit();
+  }
+  WS ws;
+  bool fresh = true;
+  int stage = 0, ahead = STAGES - 1, segment = 0;
+  for (int64_t at = lo; at < hi; ++at) {
+    if (at + STAGES - 1 < hi) {
+      if (STAGES > 1) in.next(c, a.pos, LY::chunk, heads);
+      issue(in, ahead);
+    }
+    cp_async_commit();
+    const int sub = cur.hg % a.NS, h0 = cur.hg / a.NS * a.G + sub * kGMaxGroup, nh = min(kGMaxGroup, a.G - sub * kGMaxGroup);
+    if (fresh) {
+      ws.reset();
+      ws.load_q(reinterpret_cast<const T*>(a.q) + ((int64_t)cur.b * a.Hq + h0) * D, nh, a.scale_log2);
+      fresh = false;
+    }
+    cp_async_wait<STAGES - 1>();
+    __syncwarp();
+    const int key0 = cur.k * LY::chunk + warp * kSlice;
+    if (key0 < cur.len) {
+      const int row = lane >> 2;
+      ws.step(ring + stage * Slice<D>::bytes, (key0 + row < cur.len ? 3u : 0u) | (key0 + row + 8 < cur.len ? 12u : 0u));
+    }
+    __syncwarp();                                            // the stage is free for the copy the next trip issues
+    stage = stage + 1 == STAGES ? 0 : stage + 1;
+    ahead = ahead + 1 == STAGES ? 0 : ahead + 1;
+    if (cur.k + 1 == cur.n || at + 1 == hi) {
+      // ---- the end of this block's share of (sequence, KV head, group): the warps meet
+      const bool whole = cur.k + 1 == cur.n && at - lo >= cur.n - 1;
+      ws.store(mg + warp * (kGMaxGroup * WS::kRow));
+      __syncthreads();
+      float* part = partial + (int64_t)(2 * blockIdx.x + (segment > 0)) * kPartial<D>;
+      for (int e = tid; e < nh * D; e += WARPS * 32) {
+        const int g = e / D, p = e % D;
+        const float* src = mg + g * WS::kRow;
+        float mx = -CUDART_INF_F, lt = 0.f, ot = 0.f;
+#pragma unroll
+        for (int w = 0; w < WARPS; ++w) mx = fmaxf(mx, src[w * (kGMaxGroup * WS::kRow) + D]);
+#pragma unroll
+        for (int w = 0; w < WARPS; ++w) {
+          const float* sw = src + w * (kGMaxGroup * WS::kRow);
+          const float f = weight(sw[D], mx);
+          lt += sw[D + 1] * f;
+          ot += sw[p] * f;
+        }
+        if (whole) {
+          const int64_t h = (int64_t)cur.b * a.Hq + h0 + g;
+          put(reinterpret_cast<T*>(a.O) + h * D + WS::dim_at(p), lt == 0.f ? 0.f : ot / lt);
+          if (p == 0) a.lse[h] = lse_of(mx, lt);
+        } else {
+          part[e] = ot;
+          if (p == 0) { part[kGMaxGroup * D + g] = mx; part[kGMaxGroup * (D + 1) + g] = lt; }
+        }
+      }
+      __syncthreads();                                       // before the next end overwrites the rows
+      ++segment;
+      fresh = true;
+    }
+    if (at + 1 < hi) cur.next(c, a.pos, LY::chunk, heads);
+  }
+}
+
+// Joins the partial results of one (sequence, KV head, group) and head; nothing to do where one block had all its keys.
+// grid: head of the group fastest, then (KV head, group), then sequence.
+template <typename T, int D>
+__global__ void __launch_bounds__(256)
+cache_join_kernel(CacheDecode a, DamCacheView c, const float* __restrict__ partial, int chunk, int shares) {
+  dam_chain_prologue();
+  constexpr int TD = D / 4, WAYS = 256 / TD;                 // threads of a row (4 dimensions each), partial results at a time
+  __shared__ float red[WAYS][D];
+  const int heads = c.Hkv * a.NS, per = min(a.G, kGMaxGroup);
+  const int g = blockIdx.x % per, hg = blockIdx.x / per % heads, b = blockIdx.x / per / heads;
+  const int sub = hg % a.NS, nh = min(kGMaxGroup, a.G - sub * kGMaxGroup);
+  const int tid = threadIdx.x, lane = tid & 31, way = tid / TD, col = tid % TD;
+  const int n = chunks_of(c, a.pos, b, chunk);
+  if (g >= nh || n == 0) return;
+  int64_t sum = 0, before = 0;
+  for (int x = lane; x < c.num_seqs; x += 32) {
+    const int m = chunks_of(c, a.pos, x, chunk);
+    sum += m;
+    before += x < b ? m : 0;
+  }
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
+    before += __shfl_xor_sync(0xFFFFFFFFu, before, o);
+  }
+  const int64_t total = sum * heads, first = before * heads + (int64_t)hg * n, last = first + n - 1;
+  auto share_of = [&](int64_t at) -> int {
+    int s = (int)(at * shares / total);
+    while (s + 1 < shares && share_begin(total, s + 1, shares) <= at) ++s;
+    while (s > 0 && share_begin(total, s, shares) > at) --s;
+    return s;
+  };
+  const int s0 = share_of(first), s1 = share_of(last);
+  if (s0 == s1) return;
+  float mx = -CUDART_INF_F, lt = 0.f;
+  float4 ot = make_float4(0.f, 0.f, 0.f, 0.f);
+  // (a share without a chunk lies between others when there are fewer chunks than shares; its range is empty)
+  auto row_of = [&](int s) -> const float* {
+    const int64_t lo = share_begin(total, s, shares);
+    if (lo == share_begin(total, s + 1, shares)) return nullptr;
+    return partial + (int64_t)(2 * s + (lo < first)) * kPartial<D>;
+  };
+  for (int s = s0 + lane; s <= s1; s += 32) {
+    const float* r = row_of(s);
+    if (r) mx = fmaxf(mx, r[kGMaxGroup * D + g]);
+  }
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xFFFFFFFFu, mx, o));
+#pragma unroll 4
+  for (int s = s0 + way; s <= s1; s += WAYS) {
+    const float* r = row_of(s);
+    if (!r) continue;
+    const float f = weight(r[kGMaxGroup * D + g], mx);
+    const float4 v = *reinterpret_cast<const float4*>(r + g * D + 4 * col);
+    lt += r[kGMaxGroup * (D + 1) + g] * f;
+    ot.x += v.x * f; ot.y += v.y * f; ot.z += v.z * f; ot.w += v.w * f;
+  }
+  __shared__ float sums[WAYS];
+  *reinterpret_cast<float4*>(&red[way][4 * col]) = ot;
+  if (col == 0) sums[way] = lt;
+  __syncthreads();
+  if (tid < D) {
+    float o = 0.f, l = 0.f;
+#pragma unroll
+    for (int w = 0; w < WAYS; ++w) { o += red[w][tid]; l += sums[w]; }
+    const int64_t h = (int64_t)b * a.Hq + hg / a.NS * a.G + sub * kGMaxGroup + g;
+    put(reinterpret_cast<T*>(a.O) + h * D + WarpState<T, D, DAM_CODE_INT8>::dim_at(tid), l == 0.f ? 0.f : o / l);
+    if (tid == 0) a.lse[h] = lse_of(mx, l);
+  }
+}
+
+// ---- the keys of the stored patterns ------------------------------------------------------------
+// As decode_group_kernel (dam_decode_mma.cu): one block, or a cluster of two to eight, per (sequence, KV head, group of 8 heads)
+// expands the patterns of its heads into one key list and deals its slices of 16 keys to the warps.
+constexpr int kMWarps = 5, kMStages = 2, kMBlocks = 4;
+
+template <int D>
+struct MaskedLayout {
+  static constexpr int ring = kMWarps * kMStages * Slice<D>::bytes;
+  static constexpr int merge = (kMWarps + 1) * kGMaxGroup * (D + 4) * 4;        // the merge reuses the ring
+  static constexpr int codes_off = ring > merge ? ring : merge;                 // u16 per listed key: round-local word * 32 + bit
+  static constexpr int words_off = codes_off + kGRoundWords * 32 * 2;           // u32 [head][round-local word]
+  static constexpr int total = words_off + kGMaxGroup * kGRoundWords * 4;
+};
+
+template <typename T, int D, int CODE, bool CLUSTER>
+__global__ void __launch_bounds__(kMWarps * 32, sizeof(T) == 4 ? 3 : kMBlocks)
+cache_decode_masked_kernel(CacheDecode a, DamCacheView c, const unsigned char* __restrict__ blob) {
+  dam_chain_prologue();
+  using LY = MaskedLayout<D>;
+  using WS = WarpState<T, D, CODE>;
+  constexpr int kThreads = kMWarps * 32;
+  extern __shared__ __align__(128) unsigned char sm[];
+  __shared__ int warp_tot[kMWarps];
+  unsigned short* codes = reinterpret_cast<unsigned short*>(sm + LY::codes_off);
+  uint32_t* whs = reinterpret_cast<uint32_t*>(sm + LY::words_off);
+  const int nsplit = CLUSTER ? (int)cooperative_groups::this_cluster().num_blocks() : 1;
+  const int split = CLUSTER ? (int)cooperative_groups::this_cluster().block_rank() : 0;
+  const int heads = c.Hkv * a.NS, unit = blockIdx.x / nsplit, hg = unit % heads, b = unit / heads;
+  const int kvh = hg / a.NS, sub = hg % a.NS, h0 = kvh * a.G + sub * kGMaxGroup, nh = min(kGMaxGroup, a.G - sub * kGMaxGroup);
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, row = lane >> 2, quad = lane & 3;
+  const DamHeader* H = reinterpret_cast<const DamHeader*>(blob);
+  const int pos = __ldg(a.pos + b), cu0 = __ldg(c.cu + b), cu1 = __ldg(c.cu + b + 1);
+  const bool bad_blob = H->magic != DAM_MAGIC || H->num_seqs != c.num_seqs || H->num_q_heads != a.Hq;
+  const bool bad = bad_blob || pos < 0 || pos >= cu1 - cu0;
+  T* O = reinterpret_cast<T*>(a.O) + ((int64_t)b * a.Hq + h0) * D;
+  float* lse = a.lse + (int64_t)b * a.Hq + h0;
+  if (blockIdx.x == 0) {
+    bool any = bad_blob;
+    for (int x = tid; x < c.num_seqs; x += kThreads) any |= chunks_of(c, a.pos, x, 1) == 0;
+    const int st = __syncthreads_or(any) ? (int)DAM_ERR_INVALID_ARGUMENT : 0;
+    if (tid < 64) a.scratch[tid] = tid == 1 ? (uint32_t)st : 0u;
+  }
+  if (bad) {
+    if (split == 0) {
+      for (int t = tid; t < nh * D; t += kThreads) put(O + t, 0.f);
+      if (tid < nh) lse[tid] = -CUDART_INF_F;
+    }
+    return;                                                  // (all blocks of a cluster)
+  }
+  const DamSeq sq = reinterpret_cast<const DamSeq*>(blob + H->off_seq)[b];
+  const int L = sq.L, W = sq.W;
+  const bool in_window = pos < L;
+  const int nwords = in_window ? W : 2 * W;
+  const unsigned char* Kb = c.k + (int64_t)cu0 * c.kst + (int64_t)kvh * c.ksh;
+  const unsigned char* Vb = c.v + (int64_t)cu0 * c.vst + (int64_t)kvh * c.vsh;
+  const int64_t row0 = (cu0 >> c.shift) + b;
+  WS ws;
+  ws.reset();
+  ws.load_q(reinterpret_cast<const T*>(a.q) + ((int64_t)b * a.Hq + h0) * D, nh, a.scale_log2);
+  const uint32_t ring = static_cast<uint32_t>(__cvta_generic_to_shared(sm)) + warp * (kMStages * Slice<D>::bytes);
+  const uint64_t stream_policy = l2_evict_first_policy(), keep_policy = l2_evict_last_policy();
+  for (int w0 = 0; w0 < nwords; w0 += kGRoundWords) {
+    const int total = expand_round<kMWarps>(blob, H, sq, h0, nh, in_window, pos, w0, nwords, codes, whs, warp_tot, keep_policy);
+    auto key_of = [&](uint32_t code) -> int {
+      const int w = w0 + (int)(code >> 5), k = (int)(code & 31u);
+      return (in_window || w < W) ? 32 * w + k : pos - (32 * (w - W) + k);
+    };
+    const int nslices = (total + kSlice - 1) / kSlice, first = split * kMWarps + warp, step = nsplit * kMWarps;
+    auto issue = [&](int s, int stage) {
+      const uint32_t dst = ring + stage * Slice<D>::bytes;
+#pragma unroll
+      for (int i = 0; i < kSlice * Slice<D>::pieces / 32; ++i) {
+        const int x = lane + 32 * i, r = x / Slice<D>::pieces, piece = x % Slice<D>::pieces, idx = s * kSlice + r;
+        const int j = key_of(codes[idx < total ? idx : s * kSlice]);    // places past the end repeat the slice's first key (not kept below)
+        const uint32_t at = Slice<D>::at(r, piece);
+        cp_async16(dst + at, Kb + (int64_t)j * c.kst + piece * 16, stream_policy);
+        cp_async16(dst + Slice<D>::v_off + at, Vb + (int64_t)j * c.vst + piece * 16, stream_policy);
+      }
+      const int idx = s * kSlice + (lane & 15), j = key_of(codes[idx < total ? idx : s * kSlice]);
+      cp_async4_zfill(dst + Slice<D>::scale_off + 4 * lane, (lane < 16 ? c.ks : c.vs) + (row0 + (j >> c.shift)) * c.Hkv + kvh, 4u);
+    };
+#pragma unroll
+    for (int s = 0; s < kMStages - 1; ++s) {
+      if (first + s * step < nslices) issue(first + s * step, s);
+      cp_async_commit();
+    }
+    int it = 0;
+    for (int s = first; s < nslices; s += step, ++it) {
+      if (s + (kMStages - 1) * step < nslices) issue(s + (kMStages - 1) * step, (it + kMStages - 1) % kMStages);
+      cp_async_commit();
+      cp_async_wait<kMStages - 1>();
+      __syncwarp();
+      uint32_t keep = 0u;
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        const int idx = s * kSlice + row + 8 * k;
+        if (idx < total) {
+          const uint32_t code = codes[idx];
+#pragma unroll
+          for (int e = 0; e < 2; ++e) keep |= (whs[(2 * quad + e) * kGRoundWords + (code >> 5)] >> (code & 31u) & 1u) << (2 * k + e);
+        }
+      }
+      ws.step(ring + it % kMStages * Slice<D>::bytes, keep);
+      __syncwarp();                                          // the stage is free for the copy the next trip issues
+    }
+    cp_async_wait<0>();                                      // (only empty groups are left; the merge reuses the ring)
+  }
+  // ---- merge: the warps of the block, then the blocks of the cluster
+  __syncthreads();
+  float* mg = reinterpret_cast<float*>(sm);
+  ws.store(mg + warp * (kGMaxGroup * WS::kRow));
+  __syncthreads();
+  float* folded = mg + kMWarps * kGMaxGroup * WS::kRow;
+  for (int e = tid; e < nh * D; e += kThreads) {
+    const int g = e / D, p = e % D;
+    const float* src = mg + g * WS::kRow;
+    float mx = -CUDART_INF_F, lt = 0.f, ot = 0.f;
+#pragma unroll
+    for (int w = 0; w < kMWarps; ++w) mx = fmaxf(mx, src[w * (kGMaxGroup * WS::kRow) + D]);
+#pragma unroll
+    for (int w = 0; w < kMWarps; ++w) {
+      const float* sw = src + w * (kGMaxGroup * WS::kRow);
+      const float f = weight(sw[D], mx);
+      lt += sw[D + 1] * f;
+      ot += sw[p] * f;
+    }
+    if constexpr (CLUSTER) {
+      folded[g * WS::kRow + p] = ot;
+      if (p == 0) { folded[g * WS::kRow + D] = mx; folded[g * WS::kRow + D + 1] = lt; }
+    } else {
+      put(O + g * D + WS::dim_at(p), lt == 0.f ? 0.f : ot / lt);
+      if (p == 0) lse[g] = lse_of(mx, lt);
+    }
+  }
+  if constexpr (CLUSTER) {
+    cooperative_groups::cluster_group cl = cooperative_groups::this_cluster();
+    cl.sync();
+    for (int e = split * kThreads + tid; e < nh * D; e += nsplit * kThreads) {
+      const int g = e / D, p = e % D;
+      float mv[kGMaxSplit], lv[kGMaxSplit], ov[kGMaxSplit], mx = -CUDART_INF_F;
+#pragma unroll
+      for (int k = 0; k < kGMaxSplit; ++k) {
+        mv[k] = -CUDART_INF_F; lv[k] = ov[k] = 0.f;
+        if (k < nsplit) {
+          const float* src = cl.map_shared_rank(folded, k) + g * WS::kRow;
+          mv[k] = src[D]; lv[k] = src[D + 1]; ov[k] = src[p];
+        }
+        mx = fmaxf(mx, mv[k]);
+      }
+      float lt = 0.f, ot = 0.f;
+#pragma unroll
+      for (int k = 0; k < kGMaxSplit; ++k) {
+        const float f = weight(mv[k], mx);
+        lt += lv[k] * f;
+        ot += ov[k] * f;
+      }
+      put(O + g * D + WS::dim_at(p), lt == 0.f ? 0.f : ot / lt);
+      if (p == 0) lse[g] = lse_of(mx, lt);
+    }
+    cl.sync();                                               // the folded rows stay until every block has read them
+  }
+}
+
+// Blocks per (sequence, KV head, group): as for a bf16 cache (decode_split in dam_decode_mma.cu, where it is measured).
+int masked_split(int64_t units, int sm_count) {
+  if (units * 8 <= 3 * sm_count) return 8;
+  if (units * 16 <= 15 * sm_count) return 4;
+  if (units <= 2 * sm_count) return 2;
+  return 1;
+}
+
+// the shared memory a kernel wants, asked for once per device (KEY: a set-up step of its own per instance)
+template <auto KERNEL, int BYTES>
+cudaError_t opt_in(int key, int* sm_count) {
+  int dev = 0;
+  DamDeviceInfo di;
+  const cudaError_t e = dam_current_device(&dev, &di);
+  if (e != cudaSuccess) return e;
+  *sm_count = di.sm_count;
+  if (di.smem_optin < BYTES) return cudaErrorNotSupported;
+  return dam_device_table().once(dev, key, [](void) -> cudaError_t { return cudaFuncSetAttribute(KERNEL, cudaFuncAttributeMaxDynamicSharedMemorySize, BYTES); });
+}
+
+// instance number of <T, D, CODE>
+template <typename T, int D, int CODE> constexpr int kInstance = (sizeof(T) == 4) * 4 + (D == 128) * 2 + CODE;
+
+template <typename T, int D, int CODE>
+cudaError_t launch_dense(const CacheDecode& a, const DamCacheView& c, const dam_cache_t* cache, cudaStream_t st) {
+  constexpr int WARPS = 8, STAGES = D == 128 ? 5 : 8;
+  using LY = DenseLayout<D, WARPS, STAGES>;
+  int sms = 0;
+  cudaError_t e = opt_in<cache_decode_kernel<T, D, CODE, WARPS, STAGES>, LY::total>(DAM_SETUP_CACHE_SMEM + kInstance<T, D, CODE>, &sms);
+  if (e != cudaSuccess) return e;
+  // no more shares than there can be chunks
+  const int64_t heads = (int64_t)c.Hkv * a.NS;
+  int64_t most = 0, longest = 0;
+  for (int b = 0; b < c.num_seqs; ++b) {
+    const int64_t n = ((int64_t)cache->cu_seqlens_host[b + 1] - cache->cu_seqlens_host[b] + LY::chunk - 1) / LY::chunk;
+    most += n * heads;
+    longest = n > longest ? n : longest;
+  }
+  int shares = sms < kMaxShares ? sms : kMaxShares;
+  if (most < shares) shares = most > 0 ? (int)most : 1;
+  float* partial = reinterpret_cast<float*>(a.scratch + 64);
+  e = dam_launch_chained(cache_decode_kernel<T, D, CODE, WARPS, STAGES>, dim3((unsigned)shares), dim3(WARPS * 32), LY::total, st, a, c, partial);
+  if (e != cudaSuccess || shares == 1 || longest <= 1) return e;   // (then every sequence is whole in one block)
+  const int64_t grid = heads * (a.G < kGMaxGroup ? a.G : kGMaxGroup) * c.num_seqs;
+  if (grid > 0x7FFFFFFF) return cudaErrorNotSupported;
+  return dam_launch_chained(cache_join_kernel<T, D>, dim3((unsigned)grid), dim3(256), 0, st, a, c, (const float*)partial, LY::chunk, shares);
+}
+
+template <typename T, int D, int CODE>
+cudaError_t launch_masked(const CacheDecode& a, const DamCacheView& c, const void* mask, cudaStream_t st) {
+  using LY = MaskedLayout<D>;
+  int sms = 0;
+  cudaError_t e = opt_in<cache_decode_masked_kernel<T, D, CODE, false>, LY::total>(DAM_SETUP_CACHE_SMEM + 8 + kInstance<T, D, CODE>, &sms);
+  if (e == cudaSuccess) e = opt_in<cache_decode_masked_kernel<T, D, CODE, true>, LY::total>(DAM_SETUP_CACHE_SMEM + 16 + kInstance<T, D, CODE>, &sms);
+  if (e != cudaSuccess) return e;
+  const int64_t units = (int64_t)c.num_seqs * c.Hkv * a.NS;
+  const int split = masked_split(units, sms);
+  if (units * split > 0x7FFFFFFF) return cudaErrorNotSupported;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)(units * split)); cfg.blockDim = dim3(kMWarps * 32); cfg.dynamicSmemBytes = LY::total; cfg.stream = st;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = (unsigned)split; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr; cfg.numAttrs = split > 1 ? 2 : 1;
+  return cudaLaunchKernelEx(&cfg, split > 1 ? cache_decode_masked_kernel<T, D, CODE, true> : cache_decode_masked_kernel<T, D, CODE, false>, a, c,
+                            reinterpret_cast<const unsigned char*>(mask));
+}
+
+template <typename T, int D, int CODE>
+cudaError_t launch(const CacheDecode& a, const dam_cache_t* cache, const void* mask, cudaStream_t st) {
+  const DamCacheView c = dam_cache_view(cache);
+  return mask ? launch_masked<T, D, CODE>(a, c, mask, st) : launch_dense<T, D, CODE>(a, c, cache, st);
+}
+
+}  // namespace
+
+size_t dam_cache_scratch_bytes(int head_dim) {
+  return 256 + 2ull * kMaxShares * 4 * (head_dim == 128 ? kPartial<128> : kPartial<64>);
+}
+
+cudaError_t dam_launch_cache_decode(const void* q, const dam_cache_t* cache, const void* mask, const int32_t* positions, int Hq, int dtype,
+                                    float scale, void* O, float* lse, void* scratch, cudaStream_t st) {
+  const int G = Hq / cache->num_kv_heads;
+  const CacheDecode a = {q, positions, Hq, G, (G + kGMaxGroup - 1) / kGMaxGroup, scale * 1.4426950408889634f, O, lse,
+                         reinterpret_cast<uint32_t*>(scratch)};
+  return DAM_CACHE_DISPATCH(launch, dtype, cache->head_dim, cache->code, a, cache, mask, st);
+}

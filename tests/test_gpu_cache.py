@@ -1,0 +1,475 @@
+"""The KV cache held in 8 bits on the GPU: writes bit for bit, reads bit for bit, attention against float64."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import dam_oracle as orc
+from paper_2506_11104_b200 import binding as B
+from tests import cache_reference as R
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+BF16, F32 = torch.bfloat16, torch.float32
+
+
+def _cu(lengths):
+    return [0] + [int(x) for x in np.cumsum(lengths)]
+
+
+def _ints(values):
+    return torch.tensor(values, dtype=torch.int32, device=DEV)
+
+
+def _rows(rng, n, Hkv, d, dtype, spread=1.0):
+    """Rows whose channels have sizes of their own."""
+    x = rng.standard_normal((n, Hkv, d)) * np.exp(spread * rng.standard_normal((1, Hkv, d)))
+    return torch.from_numpy(x).to(torch.float32).to(dtype).to(DEV)
+
+
+class Pair:
+    """A cache on the device and its restatement on the host, written side by side."""
+
+    def __init__(self, lengths, Hkv, d, code, block, dtype, head_major=False):
+        self.Hkv, self.d, self.dtype = Hkv, d, dtype
+        T = sum(lengths)
+        kind = B.CACHE_CODES[code][1]
+
+        def codes():
+            if head_major:
+                return torch.full((Hkv, T, d), 0x55, dtype=torch.uint8, device=DEV).view(kind).permute(1, 0, 2)
+            return torch.full((T, Hkv, d), 0x55, dtype=torch.uint8, device=DEV).view(kind)
+
+        self.cache = B.make_cache(_cu(lengths), Hkv, d, code, block, DEV, codes(), codes())
+        self.k, self.v = R.unpack(self.cache, "k"), R.unpack(self.cache, "v")
+
+    def write(self, xk, xv, counts, starts, on_device=True):
+        tokens = B.make_shape(_cu(counts), self.Hkv, self.Hkv, self.d, self.dtype, DEV, k_strides=xk.stride()[:2], v_strides=xv.stride()[:2])
+        scratch = B.dam_cache_write(xk, xv, tokens, self.cache, _ints(starts) if on_device else None)
+        assert B.dam_poll_status(scratch) == 0
+        at = 0
+        for b, (n, s) in enumerate(zip(counts, starts)):
+            for side, x in ((self.k, xk), (self.v, xv)):
+                side[b].write(x[at:at + n].cpu().double().numpy(), s)
+            at += n
+
+    def check(self):
+        for name, want in (("k", self.k), ("v", self.v)):
+            for got, w in zip(R.unpack(self.cache, name), want):
+                assert np.array_equal(got.scales, w.scales, equal_nan=True)
+                assert np.array_equal(got.codes, w.codes)
+
+    def check_read(self, starts, counts):
+        tokens = B.make_shape(_cu(counts), self.Hkv, self.Hkv, self.d, self.dtype, DEV)
+        K, V, scratch = B.dam_cache_read(self.cache, tokens, _ints(starts))
+        assert B.dam_poll_status(scratch) == 0
+        for got, side in ((K, self.k), (V, self.v)):
+            want = np.concatenate([s.read(p, n) for s, p, n in zip(side, starts, counts)])
+            want = torch.from_numpy(want).to(self.dtype)
+            assert torch.equal(torch.nan_to_num(got.cpu().float(), nan=1e30), torch.nan_to_num(want.float(), nan=1e30))
+
+
+FORMS = [(Hkv, d, dtype, code, block) for Hkv, d, dtype, code, block in
+         [(2, 128, BF16, "int8", 64), (2, 128, BF16, "e4m3", 64), (3, 64, BF16, "int8", 16), (1, 64, BF16, "e4m3", 128),
+          (2, 128, F32, "int8", 128), (1, 128, F32, "e4m3", 16), (2, 64, F32, "int8", 32), (5, 64, F32, "e4m3", 64),
+          (1, 128, BF16, "int8", 32), (1, 128, BF16, "e4m3", 128), (1, 64, BF16, "int8", 64)]]
+
+
+@pytest.mark.parametrize("Hkv,d,dtype,code,block", FORMS)
+def test_write_and_read_bit_for_bit(Hkv, d, dtype, code, block):
+    """A prompt (ragged, one sequence empty), a chunk that ends and begins inside blocks, single tokens that raise scales."""
+    rng = np.random.default_rng(5)
+    lengths = [300, 0, 129, 1, 700]
+    p = Pair(lengths, Hkv, d, code, block, dtype)
+    at = [150, 0, 127, 0, 333]
+    p.write(_rows(rng, sum(at), Hkv, d, dtype), _rows(rng, sum(at), Hkv, d, dtype), at, [0] * 5, on_device=False)
+    p.check()
+    for counts in ([1, 0, 1, 1, 1], [70, 0, 0, 0, 129], [1, 0, 1, 0, 1], [2, 0, 0, 0, 1], [1, 0, 0, 0, 5]):
+        gain = 1.3                                            # (later tokens are larger: most of them raise their block's scale)
+        xk, xv = _rows(rng, sum(counts), Hkv, d, dtype) * gain, _rows(rng, sum(counts), Hkv, d, dtype) * gain
+        p.write(xk, xv, counts, at)
+        at = [a + n for a, n in zip(at, counts)]
+        p.check()
+    p.check_read([0, 0, 0, 0, 0], [a for a in at])
+    p.check_read([17, 0, 100, 0, 64], [100, 0, 1, 1, 333])
+
+
+def test_values_on_the_border_of_two_codes_and_at_the_ends_of_the_range():
+    """Quotients of exactly k + 1/2, blocks of zeros, of the smallest and of the largest numbers."""
+    d, block = 128, 16
+    for dtype in (BF16, F32):
+        for code in ("int8", "e4m3"):
+            x = torch.zeros(16 * 7, 1, d, dtype=torch.float64)
+            x[:16] = (torch.arange(16 * d).view(16, 1, d) % 255 - 127) / 2                # amax 63.5: code k is x = k / 2, and x = k / 4 ties
+            x[0, 0, 0] = 63.5
+            x[16:32] = torch.randint(-254, 255, (16, 1, d), generator=torch.Generator().manual_seed(1)) / 4
+            x[16, 0, 5] = 63.5
+            x[48:64] = 1e-38 * torch.randn(16, 1, d, generator=torch.Generator().manual_seed(2), dtype=torch.float64)
+            x[64:80] = 3e38 * torch.rand(16, 1, d, generator=torch.Generator().manual_seed(3), dtype=torch.float64)
+            x[80:96] = 2.0 ** -133 * (torch.arange(d) % 3 - 1)                             # (bf16's smallest number)
+            x[96:112] = torch.linspace(-480, 480, 16 * d, dtype=torch.float64).view(16, 1, d)   # all e4m3 borders: amax rounds up to 512
+            x = x.to(torch.float32).to(dtype).to(DEV)
+            p = Pair([112], 1, d, code, block, dtype)
+            p.write(x, x.flip(2).contiguous(), [112], [0])
+            p.check()
+            p.check_read([0], [112])
+
+
+@pytest.mark.parametrize("code", ["int8", "e4m3"])
+@pytest.mark.parametrize("bad", [math.inf, -math.inf, math.nan])
+def test_a_block_with_an_infinity_or_a_nan_has_no_scale_until_it_is_begun_anew(code, bad):
+    rng = np.random.default_rng(7)
+    p = Pair([128], 2, 64, code, 32, BF16)
+    x, y = _rows(rng, 100, 2, 64, BF16), _rows(rng, 100, 2, 64, BF16)
+    x[40, 1, 3] = bad
+    p.write(x, y, [100], [0])
+    p.check()
+    p.check_read([0], [100])
+    assert math.isnan(p.k[0].scales[1, 1]) and np.isfinite(p.k[0].scales[1, 0]) and np.isfinite(p.v[0].scales).all()
+    one = _rows(rng, 1, 2, 64, BF16)
+    p.write(one, one, [1], [50])                              # a further token of that block: still none
+    assert math.isnan(p.k[0].scales[1, 1])
+    p.check()
+    p.write(x[:32], y[:32], [32], [32])                       # begun anew
+    p.check()
+    assert np.isfinite(p.k[0].scales).all()
+    one[0, 0, 0] = bad                                        # and one that arrives in a block that was fine
+    p.write(one, y[:1], [1], [64 + 7])
+    p.check()
+    p.check_read([0], [72])
+
+
+def test_rows_with_strides_and_codes_by_head():
+    rng = np.random.default_rng(9)
+    p = Pair([200, 90], 3, 64, "int8", 64, BF16, head_major=True)
+    wide = _rows(rng, 2 * 150, 6, 64, BF16)
+    xk, xv = wide[::2, ::2], wide.permute(1, 0, 2).contiguous().permute(1, 0, 2)[150:, 3:]
+    p.write(xk, xv, [100, 50], [30, 40])
+    p.check()
+    # packed rows into strided outputs; what lies between them stays
+    out = torch.full((150, 5, 64), 7.0, dtype=BF16, device=DEV)
+    tokens = B.make_shape([0, 100, 150], 3, 3, 64, BF16, DEV, k_strides=out.stride()[:2], v_strides=out.stride()[:2])
+    other = out.clone()
+    B.dam_cache_read(p.cache, tokens, _ints([30, 40]), out[:, 1:], other)
+    want = torch.from_numpy(np.concatenate([p.k[0].read(30, 100), p.k[1].read(40, 50)])).to(BF16)
+    assert torch.equal(out[:, 1:4].cpu(), want) and (out[:, 0] == 7).all() and (out[:, 4] == 7).all()
+    assert (other[:, 3:] == 7).all()
+
+
+def test_ranges_outside_the_capacity_are_refused_alone():
+    rng = np.random.default_rng(11)
+    p = Pair([64, 64, 64, 64], 1, 64, "e4m3", 16, BF16)
+    x = _rows(rng, 40, 1, 64, BF16)
+    tokens = B.make_shape([0, 10, 20, 30, 40], 1, 1, 64, BF16, DEV)
+    scratch = B.dam_cache_write(x, x, tokens, p.cache, _ints([-1, 55, 54, 2 ** 31 - 1]))
+    assert B.dam_poll_status(scratch) == 1
+    for side in (p.k, p.v):
+        side[2].write(x[20:30].cpu().double().numpy(), 54)
+    p.check()
+    K, V, scratch = B.dam_cache_read(p.cache, tokens, _ints([-1, 55, 54, 2 ** 31 - 1]))
+    assert B.dam_poll_status(scratch) == 1
+    assert not K[:20].any() and not K[30:].any() and not V[:20].any()
+    assert torch.equal(K[20:30].cpu(), torch.from_numpy(p.k[2].read(54, 10)).to(BF16))
+    # an empty range is none, wherever it says it starts
+    none = B.make_shape([0, 0, 0, 0, 0], 1, 1, 64, BF16, DEV)
+    assert B.dam_poll_status(B.dam_cache_write(x, x, none, p.cache, _ints([-1, 99, 0, 0]))) == 0
+    p.check()
+
+
+def test_many_sequences():
+    """More sequences than a search step looks at; most of them short or empty."""
+    rng = np.random.default_rng(13)
+    lengths = [int(n) for n in rng.integers(0, 40, size=1500)]
+    p = Pair(lengths, 1, 64, "int8", 16, BF16)
+    counts = [int(rng.integers(0, n + 1)) for n in lengths]
+    starts = [int(rng.integers(0, n - c + 1)) // 16 * 16 for n, c in zip(lengths, counts)]
+    x = _rows(rng, sum(counts), 1, 64, BF16)
+    p.write(x, x.flip(0).contiguous(), counts, starts)
+    p.check()
+    p.check_read(starts, counts)
+
+
+# ---- attention ------------------------------------------------------------------------------------------------------
+
+
+def _filled(rng, lengths, Hkv, d, code, block, dtype, spread=0.5):
+    p = Pair(lengths, Hkv, d, code, block, dtype)
+    x, y = _rows(rng, sum(lengths), Hkv, d, dtype, spread), _rows(rng, sum(lengths), Hkv, d, dtype, spread)
+    tokens = B.make_shape(_cu(lengths), Hkv, Hkv, d, dtype, DEV)
+    assert B.dam_poll_status(B.dam_cache_write(x, y, tokens, p.cache)) == 0
+    p.k, p.v = R.unpack(p.cache, "k"), R.unpack(p.cache, "v")
+    return p
+
+
+def _check(p, q, positions, O, lse, keep=None, scale=None, heads=None):
+    """keep: (sequence, head, position) -> bool [position + 1], or None: every key."""
+    Hq, d = q.shape[1], q.shape[2]
+    scale = scale or 1.0 / math.sqrt(d)
+    got, got_l = O.cpu().double().numpy(), lse.cpu().double().numpy()
+    qh = q.cpu().double().numpy()
+    G = Hq // p.Hkv
+    worst = 0.0
+    for b, i in enumerate(positions):
+        K, V = p.k[b].values(i + 1), p.v[b].values(i + 1)
+        for h in heads or range(Hq):
+            kept = np.ones(i + 1, bool) if keep is None else keep(b, h, i)
+            want, want_l, A, S, vmax, n = R.attention(qh[b, h], K[:, h // G], V[:, h // G], kept, scale)
+            if n == 0:
+                assert not got[b, h].any() and got_l[b, h] == -math.inf
+                continue
+            tol = R.tolerance(want, A, S, vmax, n, q.dtype)
+            off = np.abs(got[b, h] - want)
+            assert (off <= tol).all(), (b, h, i, float((off / tol).max()))
+            worst = max(worst, float((off / tol).max()))
+            assert abs(got_l[b, h] - want_l) <= R.lse_tolerance(want_l, d, S, n), (b, h, got_l[b, h], want_l)
+    return worst
+
+
+DECODE = [([300, 1, 129, 77], 8, 2, 128, BF16, "int8", 64), ([300, 1, 129, 77], 8, 2, 128, BF16, "e4m3", 16),
+          ([2000, 500], 4, 1, 64, BF16, "int8", 32), ([1, 2, 15, 16, 17, 127, 128, 129], 8, 8, 64, BF16, "e4m3", 128),
+          ([900], 16, 1, 128, BF16, "int8", 64), ([513, 1025], 12, 1, 64, BF16, "e4m3", 64), ([777], 24, 8, 128, BF16, "int8", 128),
+          ([640, 333], 8, 2, 128, F32, "int8", 64), ([1500], 6, 2, 64, F32, "e4m3", 16), ([400, 3], 9, 1, 128, F32, "e4m3", 32),
+          ([6000], 8, 1, 128, BF16, "e4m3", 64)]
+
+
+@pytest.mark.parametrize("lengths,Hq,Hkv,d,dtype,code,block", DECODE)
+def test_attention_over_every_key(lengths, Hq, Hkv, d, dtype, code, block):
+    rng = np.random.default_rng(21)
+    p = _filled(rng, lengths, Hkv, d, code, block, dtype)
+    q = torch.from_numpy(rng.standard_normal((len(lengths), Hq, d))).float().to(dtype).to(DEV)
+    for positions in ([n - 1 for n in lengths], [0] * len(lengths), [n // 2 for n in lengths], [min(n - 1, 127) for n in lengths]):
+        O, lse, scratch = B.dam_cache_decode_attention(q, p.cache, _ints(positions))
+        assert B.dam_poll_status(scratch) == 0
+        _check(p, q, positions, O, lse)
+
+
+def test_attention_of_many_ragged_sequences():
+    """More sequences than a warp has lanes, more shares than chunks and more chunks than shares."""
+    rng = np.random.default_rng(23)
+    lengths = [int(n) for n in rng.integers(1, 260, size=70)] + [3000]
+    p = _filled(rng, lengths, 2, 64, "int8", 16, BF16)
+    q = torch.from_numpy(rng.standard_normal((71, 4, 64))).float().to(BF16).to(DEV)
+    positions = [n - 1 for n in lengths]
+    O, lse, scratch = B.dam_cache_decode_attention(q, p.cache, _ints(positions))
+    assert B.dam_poll_status(scratch) == 0
+    _check(p, q, positions, O, lse)
+
+
+def test_attention_does_not_depend_on_what_lies_behind_the_position():
+    """NaN codes, infinite and NaN scales behind the last token, and the next sequence's tokens, have no part in the result."""
+    rng = np.random.default_rng(25)
+    for block in (16, 128):
+        p = _filled(rng, [200, 200], 2, 128, "e4m3", block, BF16)
+        q = torch.from_numpy(rng.standard_normal((2, 8, 128))).float().to(BF16).to(DEV)
+        positions = [100, 33]
+        want = B.dam_cache_decode_attention(q, p.cache, _ints(positions))
+        for b, i in enumerate(positions):
+            t0 = 200 * b
+            for codes in (p.cache.k_codes, p.cache.v_codes):
+                codes.view(torch.uint8)[t0 + i + 1:t0 + 200] = 0x7F
+            for scales in (p.cache.k_scales, p.cache.v_scales):
+                row = t0 // block + b
+                scales[row + i // block + 1:row + -(-200 // block)] = math.nan
+        got = B.dam_cache_decode_attention(q, p.cache, _ints(positions))
+        assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
+def test_attention_with_scales_of_very_different_sizes():
+    """V blocks a factor of 1e12 apart in either order, K blocks that send logits far up: both references move."""
+    rng = np.random.default_rng(27)
+    for code in ("int8", "e4m3"):
+        for order in (1, -1):
+            p = Pair([256], 1, 64, code, 16, BF16)
+            x = torch.from_numpy(rng.standard_normal((256, 1, 64))).float()
+            size = torch.logspace(-6 * order, 6 * order, 16).repeat_interleave(16)[:, None, None]
+            grow = torch.linspace(0.1, 30, 256)[:, None, None].flip(0) if order < 0 else torch.linspace(0.1, 30, 256)[:, None, None]
+            p.write((x * grow).to(BF16).to(DEV), (x.flip(0) * size).to(BF16).to(DEV), [256], [0])
+            q = torch.from_numpy(rng.standard_normal((1, 4, 64))).float().to(BF16).to(DEV)
+            O, lse, _ = B.dam_cache_decode_attention(q, p.cache, _ints([255]))
+            _check(p, q, [255], O, lse)
+
+
+def test_queries_of_any_size_and_a_scale_of_its_own():
+    rng = np.random.default_rng(29)
+    p = _filled(rng, [150], 1, 128, "int8", 64, BF16)
+    q = torch.from_numpy(rng.standard_normal((1, 6, 128))).float()
+    q[0, 0] *= 1e-30
+    q[0, 1] *= 1e30
+    q[0, 2] = 0
+    q[0, 3, ::2] *= 1e-6                                      # elements far below the row's largest
+    q = q.to(BF16).to(DEV)
+    for scale in (0.25,):
+        O, lse, _ = B.dam_cache_decode_attention(q, p.cache, _ints([149]), softmax_scale=scale)
+        _check(p, q, [149], O, lse, scale=scale, heads=[0, 2, 3, 4, 5])
+        # logits of 1e30: the largest alone counts
+        K, V = p.k[0].values(150)[:, 0], p.v[0].values(150)[:, 0]
+        x = K @ q[0, 1].cpu().double().numpy()
+        assert np.abs(O[0, 1].cpu().double().numpy() - V[x.argmax()]).max() <= 2.0 ** -7 * np.abs(V[x.argmax()]).max()
+
+
+def test_a_nan_stays_a_nan():
+    rng = np.random.default_rng(31)
+    p = _filled(rng, [150, 150], 2, 64, "int8", 64, BF16)
+    q = torch.from_numpy(rng.standard_normal((2, 4, 64))).float().to(BF16).to(DEV)
+    q[0, 0, 5] = math.nan
+    p.cache.v_scales[150 // 64 + 1 + 1, 1] = math.nan         # a V block of sequence 1, KV head 1
+    O, lse, _ = B.dam_cache_decode_attention(q, p.cache, _ints([149, 149]))
+    assert torch.isnan(O[0, 0]).all() and torch.isnan(lse[0, 0]) and torch.isfinite(O[0, 1:].float()).all()
+    assert torch.isnan(O[1, 2:]).all() and torch.isfinite(lse[1]).all() and torch.isfinite(O[1, :2].float()).all()
+
+
+def _blob(rng, lengths, Hq, pcl, empty_head=None):
+    """A blob from planted columns and diagonals, and its masks by the oracle."""
+    maps, masks = [], []
+    for b, S in enumerate(lengths):
+        L = min(S, pcl)
+        per = []
+        for h in range(Hq):
+            P = np.zeros((L, L), np.float32)
+            if h != empty_head:
+                for c in rng.choice(L, size=min(L, int(rng.integers(0, 6))), replace=False):
+                    P[c:, c] = 1
+                for r in range(int(rng.integers(0, min(L, 40)))):
+                    P[np.arange(r, L), np.arange(0, L - r)] = 1
+                P[np.triu_indices(L, 1)] = 0
+            maps.append(P.reshape(-1))
+            per.append(orc.head_mask_from_probs(P, S, 0.3, 0.8, 0.5, 1e-8))
+        masks.append(per)
+    shape = B.make_shape(_cu(lengths), Hq, Hq, 64, BF16, DEV)
+    blob, _ = B.dam_build_masks_from_scores(torch.from_numpy(np.concatenate(maps)).to(DEV), shape, B.make_rule(pcl, 0.3, 0.8))
+    assert B.dam_poll_status(blob) == 0
+
+    def keep(b, h, i):
+        hm = masks[b][h]
+        return orc.extended_rows(hm.M, hm.D, hm.V, max(i + 1, hm.L), [i])[0, :i + 1].astype(bool)
+    return blob, keep
+
+
+@pytest.mark.parametrize("lengths,Hq,Hkv,d,dtype,code,block,pcl", [
+    ([700, 400], 8, 2, 128, BF16, "int8", 64, 128), ([700, 130, 1], 4, 4, 64, BF16, "e4m3", 16, 100),
+    ([600], 16, 1, 64, BF16, "int8", 32, 96), ([500, 300], 8, 1, 128, F32, "e4m3", 128, 128), ([640], 10, 1, 64, F32, "int8", 64, 160),
+    ([5000], 8, 1, 64, BF16, "e4m3", 64, 2112)])
+def test_attention_under_stored_patterns(lengths, Hq, Hkv, d, dtype, code, block, pcl):
+    rng = np.random.default_rng(33)
+    p = _filled(rng, lengths, Hkv, d, code, block, dtype)
+    blob, keep = _blob(rng, lengths, Hq, pcl, empty_head=1)
+    q = torch.from_numpy(rng.standard_normal((len(lengths), Hq, d))).float().to(dtype).to(DEV)
+    L = min(lengths[0], pcl)
+    for at in (0, 5, L - 1, L, L + 1, 2 * L - 1, 2 * L, 10 ** 6):
+        positions = [min(n - 1, at) for n in lengths]
+        O, lse, scratch = B.dam_cache_decode_attention(q, p.cache, _ints(positions), blob)
+        assert B.dam_poll_status(scratch) == 0
+        _check(p, q, positions, O, lse, keep)
+
+
+@pytest.mark.parametrize("num_seqs", [55, 56, 138, 139, 296, 297])
+def test_attention_under_patterns_split_over_blocks(num_seqs):
+    """Enough sequences for clusters of 8, 4, 2 and 1 blocks (both sides of every boundary on 148 SMs)."""
+    rng = np.random.default_rng(num_seqs)
+    p = _filled(rng, [200] * num_seqs, 1, 64, "int8", 16, BF16)
+    blob, keep = _blob(rng, [200] * num_seqs, 2, 96)
+    q = torch.from_numpy(rng.standard_normal((num_seqs, 2, 64))).float().to(BF16).to(DEV)
+    positions = [int(x) for x in rng.integers(0, 200, size=num_seqs)]
+    O, lse, _ = B.dam_cache_decode_attention(q, p.cache, _ints(positions), blob)
+    _check(p, q, positions, O, lse, keep)
+
+
+def test_a_key_another_head_keeps_has_no_part_in_a_head_that_does_not():
+    """Heads of one group, keys of a block without a scale: NaN for the head that keeps one, nothing for the other."""
+    rng = np.random.default_rng(35)
+    p = _filled(rng, [256], 1, 64, "int8", 16, BF16)
+    L = 64
+    P = np.zeros((2, L, L), np.float32)
+    P[0, 3:, 3] = 1                                           # head 0: column 3 alone
+    P[1, 20:, 20] = 1                                         # head 1: column 20, in the next block
+    shape = B.make_shape([0, 256], 2, 1, 64, BF16, DEV)
+    blob, _ = B.dam_build_masks_from_scores(torch.from_numpy(P.reshape(-1)).to(DEV), shape, B.make_rule(L, 0.3, 0.8))
+    p.cache.v_scales[1] = math.nan
+    p.cache.k_scales[1] = math.nan
+    q = torch.ones(1, 2, 64, dtype=BF16, device=DEV)
+    O, lse, _ = B.dam_cache_decode_attention(q, p.cache, _ints([200]), blob)
+    assert torch.isfinite(O[0, 0].float()).all() and torch.isfinite(lse[0, 0]) and torch.isnan(O[0, 1]).all()
+
+
+def test_positions_outside_the_capacity_and_foreign_blobs():
+    rng = np.random.default_rng(37)
+    p = _filled(rng, [256, 256, 256], 1, 64, "e4m3", 64, BF16)
+    q = torch.ones(3, 2, 64, dtype=BF16, device=DEV)
+    blob, _ = _blob(rng, [256, 256, 256], 2, 64)
+    for mask in (None, blob):
+        O, lse, scratch = B.dam_cache_decode_attention(q, p.cache, _ints([100, 256, -1]), mask)
+        assert B.dam_poll_status(scratch) == 1
+        assert not O[1:].any() and torch.isneginf(lse[1:]).all() and torch.isfinite(lse[0]).all()
+    other, _ = _blob(rng, [256, 256], 2, 64)                  # built for another number of sequences
+    O, lse, scratch = B.dam_cache_decode_attention(q, p.cache, _ints([100, 100, 100]), other)
+    assert B.dam_poll_status(scratch) == 1 and not O.any() and torch.isneginf(lse).all()
+
+
+def test_a_generation_step_captured_and_replayed_on_another_stream():
+    """Write the new token, attend: captured once, replayed with other tokens and positions; two graphs share one scratch."""
+    rng = np.random.default_rng(39)
+    lengths, Hq, Hkv, d = [300, 500], 8, 2, 128
+    p = Pair(lengths, Hkv, d, "int8", 64, BF16)
+    x, y = _rows(rng, 450, Hkv, d, BF16), _rows(rng, 450, Hkv, d, BF16)
+    p.write(x, y, [150, 300], [0, 0])
+    tokens = B.make_shape([0, 1, 2], Hkv, Hkv, d, BF16, DEV)
+    q = torch.zeros(2, Hq, d, dtype=BF16, device=DEV)
+    k, v = torch.zeros(2, Hkv, d, dtype=BF16, device=DEV), torch.zeros(2, Hkv, d, dtype=BF16, device=DEV)
+    pos, O = _ints([150, 300]), torch.zeros(2, Hq, d, dtype=BF16, device=DEV)
+    lse = torch.zeros(2, Hq, device=DEV)
+    wscr = torch.empty(256, dtype=torch.uint8, device=DEV)
+    scratch = torch.empty(B.dam_cache_sizes(p.cache, Hq)[1], dtype=torch.uint8, device=DEV)
+    blob, keep = _blob(rng, lengths, Hq, 96)
+    side = torch.cuda.Stream()
+    graphs = []
+    for mask in (None, blob):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=side):
+            B.dam_cache_write(k, v, tokens, p.cache, pos, wscr)
+            B.dam_cache_decode_attention(q, p.cache, pos, mask, O=O, lse=lse, scratch=scratch)
+        graphs.append(g)
+    torch.cuda.synchronize()
+    p.check()                                                 # nothing has run yet
+    for step in range(6):
+        nk, nv = _rows(rng, 2, Hkv, d, BF16) * (1 + step), _rows(rng, 2, Hkv, d, BF16)
+        nq = torch.from_numpy(rng.standard_normal((2, Hq, d))).float().to(BF16)
+        positions = [150 + step, 300 + step]
+        with torch.cuda.stream(side):
+            k.copy_(nk), v.copy_(nv), q.copy_(nq), pos.copy_(_ints(positions))
+            graphs[step % 2].replay()
+        torch.cuda.synchronize()
+        for b in range(2):
+            p.k[b].write(nk[b:b + 1].cpu().double().numpy(), positions[b])
+            p.v[b].write(nv[b:b + 1].cpu().double().numpy(), positions[b])
+        p.check()
+        assert B.dam_poll_status(wscr) == 0 and B.dam_poll_status(scratch) == 0
+        _check(p, q, positions, O, lse, keep if step % 2 else None)
+
+
+def test_prompt_chunk_and_generation_together():
+    """As a server uses them: a prompt is prefilled and written, its next chunk attends to what the cache gives back, then tokens
+    are generated under the same masks; the generation step agrees with the chunk's rows."""
+    rng = np.random.default_rng(41)
+    S, first, Hq, Hkv, d, pcl = 1024, 512, 8, 2, 128, 256
+    K, V = _rows(rng, S, Hkv, d, BF16, 0.3), _rows(rng, S, Hkv, d, BF16, 0.3)
+    Q = torch.from_numpy(rng.standard_normal((S, Hq, d))).float().to(BF16).to(DEV)
+    blob, keep = _blob(rng, [S], Hq, pcl)
+    p = Pair([S], Hkv, d, "int8", 64, BF16)
+    p.write(K[:first], V[:first], [first], [0])
+    p.write(K[first:], V[first:], [S - first], [first])
+    p.check()
+    shape = B.make_shape([0, S], Hq, Hkv, d, BF16, DEV)
+    Kc, Vc, _ = B.dam_cache_read(p.cache, shape)
+    O, lse = torch.zeros_like(Q), torch.zeros(Hq, S, device=DEV)
+    scr = B.dam_sparse_attention_rows(Q, Kc, Vc, blob, shape, [(first, S)], O, lse)
+    assert B.dam_poll_status(scr) == 0
+    for i in (first, 700, S - 1):
+        o, l, scratch = B.dam_cache_decode_attention(Q[i:i + 1], p.cache, _ints([i]), blob)
+        assert B.dam_poll_status(scratch) == 0
+        _check(p, Q[i:i + 1], [i], o, l, keep)
+        # the chunk's K and V are the cache's rounded to bf16 (2^-8), its P and O are rounded to bf16 too
+        fin = torch.isfinite(l[0])
+        assert torch.equal(torch.isfinite(lse[:, i]), fin)
+        bound = 4 * 2.0 ** -8 * float(Vc.float().abs().max())
+        assert (o[0].float() - O[i].float()).abs().max() <= bound
