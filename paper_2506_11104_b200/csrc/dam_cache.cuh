@@ -75,27 +75,48 @@ __device__ __forceinline__ float cache_scale(uint32_t amax) {
   }
 }
 
-// The code of x under the scale s (inv = 1 / s), as the low byte.
+// The codes of eight values under the scale s (inv = 1 / s).
 template <int CODE>
-__device__ __forceinline__ uint32_t cache_code(float x, float s, float inv) {
+__device__ __forceinline__ uint2 cache_codes8(const float* x, float s, float inv) {
+  uint32_t w[2];
   if constexpr (CODE == DAM_CODE_INT8) {
-    // nearest integer to x / s, ties to even, decided on the exact quotient: x * inv is off by 127 * 2^-23 at most, so q is
-    // right or, next to a border, one off; x - q s is exact there (a multiple of half an ulp of s, at most s / 2 (1 + 2^-15))
-    float q = rintf(x * inv);
-    const float r = fmaf(-q, s, x), half = 0.5f * s;
-    if (fabsf(r) >= half) {
-      const bool odd = ((int)q & 1) != 0;
-      if (r > half || (r == half && odd)) q += 1.f;
-      else if (r < -half || (r == -half && odd)) q -= 1.f;
+    // The nearest integer to x / s, ties to even, decided on the exact quotient.  x * inv + 1.5 * 2^23 is rounded to an integer
+    // q (its low byte is the code); x * inv is off by 2^-16 at most, so q is right, or one off next to a border of two codes.
+    // There |x - q s| is s / 2 or next to it, and the difference is exact: a multiple of half an ulp of s.
+    constexpr float kMagic = 12582912.f;
+    float t[8], far = 0.f;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      t[k] = fmaf(x[k], inv, kMagic);
+      far = fmaxf(far, fabsf(fmaf(-(t[k] - kMagic), s, x[k])));
     }
-    const int c = max(-127, min(127, (int)q));
-    return (uint32_t)c & 0xFFu;
+    const float half = 0.5f * s;
+    if (far >= half) {                 // (one of the eight, at most: few values are that near a border)
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        const float q = t[k] - kMagic, r = fmaf(-q, s, x[k]);
+        const bool odd = (__float_as_uint(t[k]) & 1u) != 0;
+        if (r > half || (r == half && odd)) t[k] += 1.f;
+        else if (r < -half || (r == -half && odd)) t[k] -= 1.f;
+        t[k] = fminf(fmaxf(t[k], kMagic - 127.f), kMagic + 127.f);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const uint32_t lo = __byte_perm(__float_as_uint(t[4 * i]), __float_as_uint(t[4 * i + 1]), 0x0040);
+      const uint32_t hi = __byte_perm(__float_as_uint(t[4 * i + 2]), __float_as_uint(t[4 * i + 3]), 0x0040);
+      w[i] = __byte_perm(lo, hi, 0x5410);
+    }
   } else {
     // (the scale is a power of two: x * inv is exact, or so small that its code is zero)
-    uint16_t p;
-    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(p) : "f"(0.f), "f"(x * inv));
-    return p & 0xFFu;
+    uint16_t h[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(h[i]) : "f"(x[2 * i + 1] * inv), "f"(x[2 * i] * inv));
+    w[0] = (uint32_t)h[0] | (uint32_t)h[1] << 16;
+    w[1] = (uint32_t)h[2] | (uint32_t)h[3] << 16;
   }
+  return make_uint2(w[0], w[1]);
 }
 
 // ---- which sequence -----------------------------------------------------------------------------

@@ -150,12 +150,16 @@ struct WarpState {
     qs[1] = __shfl_sync(0xFFFFFFFFu, back, 8 * quad + 4);
   }
 
-  // One slice.  keep: bit e (e + 2): head 2 quad + e keeps key row (row + 8); a key that a head does not keep has no part in it.
+  // One slice.  ALL: every head keeps every key; otherwise keep: bit e (e + 2): head 2 quad + e keeps key row (row + 8); a key that
+  // a head does not keep has no part in it.  UNIFORM: the 16 keys share their scales (they lie in one block).
+  template <bool ALL, bool UNIFORM>
   __device__ __forceinline__ void step(uint32_t slice, uint32_t keep) {
     using SL = Slice<D>;
     const int lane = threadIdx.x & 31, row = lane >> 2, quad = lane & 3;
-    const float ks0 = lds_float(slice + SL::scale_off + 4 * row), ks1 = lds_float(slice + SL::scale_off + 4 * row + 32);
-    const float vs0 = lds_float(slice + SL::scale_off + 64 + 4 * row), vs1 = lds_float(slice + SL::scale_off + 96 + 4 * row);
+    const uint32_t sc = slice + SL::scale_off + (UNIFORM ? 0 : 4 * row);
+    const float ks0 = lds_float(sc), vs0 = lds_float(sc + 64);
+    const float ks1 = UNIFORM ? ks0 : lds_float(sc + 32), vs1 = UNIFORM ? vs0 : lds_float(sc + 96);
+    auto kept = [&](int bit) { return ALL || (keep >> bit & 1u); };
     // S^T = K q^T: k-step s takes the dimensions D / 4 * quad + 4 s ... of a lane
     float st[2][4] = {};                                     // (two chains of instructions, half as long)
 #pragma unroll
@@ -175,12 +179,16 @@ struct WarpState {
     float x[4];
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
-      x[e] = keep >> e & 1u ? (st[0][e] + st[1][e]) * (ks0 * qs[e]) : -CUDART_INF_F;
-      x[2 + e] = keep >> (2 + e) & 1u ? (st[0][2 + e] + st[1][2 + e]) * (ks1 * qs[e]) : -CUDART_INF_F;
+      x[e] = kept(e) ? (st[0][e] + st[1][e]) * (ks0 * qs[e]) : -CUDART_INF_F;
+      x[2 + e] = kept(2 + e) ? (st[0][2 + e] + st[1][2 + e]) * (ks1 * qs[e]) : -CUDART_INF_F;
     }
-    // the reference moves when a logit lies more than 8 above it: probabilities stay below 2^8, and most slices move nothing
-    const bool up = fmaxf(x[0], x[2]) > m[0] + 8.f || fmaxf(x[1], x[3]) > m[1] + 8.f;
-    if (__any_sync(0xFFFFFFFFu, up)) {
+    // The reference of the logits moves when one lies more than 8 above it (probabilities stay below 2^8), that of the V scales
+    // when one reaches 128 times it: most slices move nothing.
+    float c0 = vs0 * vinv, c1 = UNIFORM ? c0 : vs1 * vinv;
+    const bool far = fmaxf(x[0], x[2]) > m[0] + 8.f || fmaxf(x[1], x[3]) > m[1] + 8.f;
+    const bool large = ((ALL || keep & 3u) && c0 > 128.f) || (!UNIFORM && (ALL || keep & 12u) && c1 > 128.f);
+    if (__any_sync(0xFFFFFFFFu, far || large)) {
+      float f[2];
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
         float mx = fmaxf(x[e], x[2 + e]);
@@ -188,23 +196,22 @@ struct WarpState {
         mx = fmaxf(mx, __shfl_xor_sync(0xFFFFFFFFu, mx, 8));
         mx = fmaxf(mx, __shfl_xor_sync(0xFFFFFFFFu, mx, 16));
         const float mn = fmaxf(m[e], mx);
-        const float alpha = mn == -CUDART_INF_F ? 1.f : g_ex2(m[e] - mn);
+        f[e] = mn == -CUDART_INF_F ? 1.f : g_ex2(m[e] - mn);
         m[e] = mn;
-        l[e] *= alpha;
-#pragma unroll
-        for (int u = 0; u < KS; ++u) { o[u][e] *= alpha; o[u][2 + e] *= alpha; }
+        l[e] *= f[e];
       }
-    }
-    // and the reference of the V scales when one of them reaches 128 times it
-    if (__any_sync(0xFFFFFFFFu, (keep & 3u && vs0 * vinv > 128.f) || (keep & 12u && vs1 * vinv > 128.f))) {
-      float top = fmaxf(keep & 3u ? vs0 : 0.f, keep & 12u ? vs1 : 0.f);
+      float top = fmaxf(ALL || keep & 3u ? vs0 : 0.f, ALL || keep & 12u ? vs1 : 0.f);
 #pragma unroll
       for (int d = 1; d < 32; d <<= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, d));
-      const int f = max(1, min(234, 260 - (int)(__float_as_uint(top) >> 23)));     // top * 2^(f - 127) lies in [64, 128)
-      const float now = __uint_as_float((uint32_t)f << 23), ratio = now / vinv;
-      vinv = now;
+      if (top * vinv > 128.f) {
+        const int n = max(1, min(234, 260 - (int)(__float_as_uint(top) >> 23)));   // top * 2^(n - 127) lies in [64, 128)
+        const float now = __uint_as_float((uint32_t)n << 23), ratio = now / vinv;
+        vinv = now;
+        c0 = vs0 * vinv; c1 = vs1 * vinv;
+        f[0] *= ratio; f[1] *= ratio;
+      }
 #pragma unroll
-      for (int u = 0; u < KS; ++u) { o[u][0] *= ratio; o[u][1] *= ratio; o[u][2] *= ratio; o[u][3] *= ratio; }
+      for (int u = 0; u < KS; ++u) { o[u][0] *= f[0]; o[u][1] *= f[1]; o[u][2] *= f[0]; o[u][3] *= f[1]; }
     }
     float w[4];
 #pragma unroll
@@ -213,8 +220,8 @@ struct WarpState {
       const float p0 = g_ex2(x[e] - ref), p1 = g_ex2(x[2 + e] - ref);
       l[e] += p0 + p1;
       // (a key that is not kept may stand in a block without a scale: 0 * NaN is not 0)
-      w[e] = keep >> e & 1u ? p0 * (vs0 * vinv) : 0.f;
-      w[2 + e] = keep >> (2 + e) & 1u ? p1 * (vs1 * vinv) : 0.f;
+      w[e] = kept(e) ? p0 * c0 : 0.f;
+      w[2 + e] = kept(2 + e) ? p1 * c1 : 0.f;
     }
     // P^T as operands (k = key, n = head): the transposes of the two 8 x 8 blocks [key][head]
     const uint32_t h0 = pack_half2(w[0], w[1]), h1 = pack_half2(w[2], w[3]);
@@ -305,59 +312,64 @@ __device__ __forceinline__ int chunks_of(const DamCacheView& c, const int32_t* p
 }
 
 // Chunks per head over all sequences (whole warp).
-__device__ __forceinline__ int64_t total_chunks(const DamCacheView& c, const int32_t* pos, int chunk) {
-  int64_t sum = 0;
+__device__ __forceinline__ int total_chunks(const DamCacheView& c, const int32_t* pos, int chunk) {
+  int sum = 0;
   for (int b = threadIdx.x & 31; b < c.num_seqs; b += 32) sum += chunks_of(c, pos, b, chunk);
-#pragma unroll
-  for (int o = 1; o < 32; o <<= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
-  return sum;
+  return __reduce_add_sync(0xFFFFFFFFu, sum);
 }
 
-// A place in the list of chunks.
+// A place in the list of chunks.  Consumers and the copies that run ahead of them walk the list each on their own.
 struct Place {
-  int b, len, n;               // sequence, its keys, its chunks per head
-  int hg, k;                   // KV head and group, chunk
-  int64_t row0;                // scale row of the sequence's first block
-  int64_t tok0;
+  int b, hg;                   // sequence; KV head and group of heads
+  int n, left;                 // chunks of the sequence, and how many are left of this (KV head, group), this one included
+  int live;                    // keys of the sequence from the warp's slice of this chunk on (may be none: <= 0)
   __device__ __forceinline__ void enter(const DamCacheView& c, const int32_t* pos, int b_, int chunk) {
     b = b_;
-    len = __ldg(pos + b) + 1;
     n = chunks_of(c, pos, b, chunk);
-    tok0 = __ldg(c.cu + b);
-    row0 = (tok0 >> c.shift) + b;
   }
-  // chunk `at` of the whole list (which has it)
-  __device__ __forceinline__ void locate(const DamCacheView& c, const int32_t* pos, int chunk, int heads, int64_t at) {
+  __device__ __forceinline__ void begin(const int32_t* pos, int chunk, int k) {
+    left = n - k;
+    live = __ldg(pos + b) + 1 - k * chunk - (int)(threadIdx.x >> 5) * kSlice;
+  }
+  // chunk `at` of the whole list (which has it); returns its number within the (KV head, group)
+  __device__ __forceinline__ int locate(const DamCacheView& c, const int32_t* pos, int chunk, int heads, int at) {
     const int lane = threadIdx.x & 31;
-    int64_t before = 0;
+    int before = 0;
     for (int base = 0; base < c.num_seqs; base += 32) {
       const int mine = base + lane < c.num_seqs ? chunks_of(c, pos, base + lane, chunk) : 0;
-      int64_t incl = mine;
+      int incl = mine;
 #pragma unroll
       for (int o = 1; o < 32; o <<= 1) {
-        const int64_t y = __shfl_up_sync(0xFFFFFFFFu, incl, o);
+        const int y = __shfl_up_sync(0xFFFFFFFFu, incl, o);
         if (lane >= o) incl += y;
       }
       const uint32_t past = __ballot_sync(0xFFFFFFFFu, (before + incl) * heads > at);
       if (past) {
         const int w = __ffs(past) - 1;
-        const int64_t first = (before + __shfl_sync(0xFFFFFFFFu, incl - mine, w)) * heads;
+        const int first = (before + __shfl_sync(0xFFFFFFFFu, incl - mine, w)) * heads;
         enter(c, pos, base + w, chunk);
-        hg = (int)((at - first) / n);
-        k = (int)((at - first) % n);
-        return;
+        hg = (at - first) / n;
+        const int k = (at - first) % n;
+        begin(pos, chunk, k);
+        return k;
       }
       before += __shfl_sync(0xFFFFFFFFu, incl, 31);
     }
-    b = len = n = hg = k = 0; row0 = tok0 = 0;
+    b = hg = 0; n = left = 1; live = 0;                       // (not reached)
+    return 0;
   }
-  // the next chunk (there is one)
-  __device__ __forceinline__ void next(const DamCacheView& c, const int32_t* pos, int chunk, int heads) {
-    if (++k < n) return;
-    k = 0;
-    if (++hg < heads) return;
-    hg = 0;
-    do { enter(c, pos, b + 1, chunk); } while (n == 0 && b + 1 < c.num_seqs);
+  // the next chunk (there is one); whether it is another (KV head, group)'s first
+  __device__ __forceinline__ bool next(const DamCacheView& c, const int32_t* pos, int chunk, int heads) {
+    if (--left > 0) {
+      live -= chunk;
+      return false;
+    }
+    if (++hg == heads) {
+      hg = 0;
+      do { enter(c, pos, b + 1, chunk); } while (n == 0 && b + 1 < c.num_seqs);
+    }
+    begin(pos, chunk, 0);
+    return true;
   }
 };
 
@@ -370,7 +382,16 @@ struct DenseLayout {
 // floats of one partial result: O of 8 heads, references, sums
 template <int D> constexpr int kPartial = kGMaxGroup * (D + 2);
 
-__device__ __forceinline__ int64_t share_begin(int64_t total, int c, int shares) { return total * c / shares; }
+// The shares of `total` chunks (below 2^31: the host sees to it): the first `more` have one chunk more than the others.
+struct Shares {
+  int each, more;
+  __device__ __forceinline__ Shares(int total, int shares) : each(total / shares), more(total % shares) {}
+  __device__ __forceinline__ int begin(int s) const { return s * each + min(s, more); }
+  __device__ __forceinline__ int of(int at) const {           // the share that has chunk `at`
+    const int there = more * (each + 1);
+    return at < there ? at / (each + 1) : more + (at - there) / each;
+  }
+};
 
 template <typename T, int D, int CODE, int WARPS, int STAGES>
 __global__ void __launch_bounds__(WARPS * 32, 1)
@@ -394,71 +415,102 @@ cache_decode_kernel(CacheDecode a, DamCacheView c, float* __restrict__ partial) 
       for (int t = tid; t < a.Hq; t += WARPS * 32) a.lse[(int64_t)b * a.Hq + t] = -CUDART_INF_F;
     }
   }
-  const int64_t total = total_chunks(c, a.pos, LY::chunk) * heads;
-  const int64_t lo = share_begin(total, blockIdx.x, shares), hi = share_begin(total, blockIdx.x + 1, shares);
-  if (lo == hi) return;
+  const Shares sh(total_chunks(c, a.pos, LY::chunk) * heads, shares);
+  const int lo = sh.begin(blockIdx.x), todo = sh.begin(blockIdx.x + 1) - lo;
+  if (todo == 0) return;
   Place in, cur;
-  in.locate(c, a.pos, LY::chunk, heads, lo);
+  const int k0 = in.locate(c, a.pos, LY::chunk, heads, lo);
   cur = in;
 
-  auto issue = [&](const Place& p, int stage) {
-    const int key0 = p.k * LY::chunk + warp * kSlice;
-    if (key0 < p.len) {
-      const int kvh = p.hg / a.NS;
-      const uint32_t dst = ring + stage * Slice<D>::bytes;
-      const unsigned char* K = c.k + (p.tok0 + key0) * c.kst + (int64_t)kvh * c.ksh;
-      const unsigned char* V = c.v + (p.tok0 + key0) * c.vst + (int64_t)kvh * c.vsh;
-      const int live = p.len - key0;                         // keys of the slice that exist; the others are filled with zeros
+  // The copies: this lane's 16-byte pieces of the slice's rows (rows lane / pieces + kRows i), and one scale (K's: lanes 0 .. 15).
+  constexpr int P = Slice<D>::pieces, kRows = 32 / P, kCopies = kSlice / kRows;
+  const int row0 = lane / P, piece = lane % P;
+  const unsigned char *kp, *vp;
+  const float* sp;                     // scale of block 0 of the sequence
+  int key;                             // first key of the slice
+  auto aim = [&](int k) {
+    const int kvh = in.hg / a.NS;
+    const int64_t cu = __ldg(c.cu + in.b);
+    key = k * LY::chunk + warp * kSlice;
+    kp = c.k + (cu + key + row0) * c.kst + (int64_t)kvh * c.ksh + piece * 16;
+    vp = c.v + (cu + key + row0) * c.vst + (int64_t)kvh * c.vsh + piece * 16;
+    sp = (lane < 16 ? c.ks : c.vs) + ((cu >> c.shift) + in.b) * c.Hkv + kvh;
+  };
+  auto issue = [&](int stage) {
+    if (in.live <= 0) return;
+    const uint32_t dst = ring + stage * Slice<D>::bytes;
+    if (in.live >= kSlice) {
 #pragma unroll
-      for (int i = 0; i < kSlice * Slice<D>::pieces / 32; ++i) {
-        const int x = lane + 32 * i, r = x / Slice<D>::pieces, piece = x % Slice<D>::pieces;
-        const int from = r < live ? r : 0;
-        const uint32_t n = r < live ? 16u : 0u, at = Slice<D>::at(r, piece);
-        cp_async16_zfill(dst + at, K + from * c.kst + piece * 16, n);
-        cp_async16_zfill(dst + Slice<D>::v_off + at, V + from * c.vst + piece * 16, n);
+      for (int i = 0; i < kCopies; ++i) {
+        const uint32_t at = Slice<D>::at(row0 + kRows * i, piece);
+        cp_async16_zfill(dst + at, kp + i * kRows * c.kst, 16u);
+        cp_async16_zfill(dst + Slice<D>::v_off + at, vp + i * kRows * c.vst, 16u);
       }
-      const int r = lane & 15, from = r < live ? r : 0;
-      const float* s = (lane < 16 ? c.ks : c.vs) + (p.row0 + ((key0 + from) >> c.shift)) * c.Hkv + kvh;
-      cp_async4_zfill(dst + Slice<D>::scale_off + 4 * lane, s, r < live ? 4u : 0u);
+    } else {                           // rows of keys that do not exist are filled with zeros
+#pragma unroll 1
+      for (int i = 0; i < kCopies; ++i) {
+        const int r = row0 + kRows * i;
+        const uint32_t n = r < in.live ? 16u : 0u, at = Slice<D>::at(r, piece);
+        const int back = r < in.live ? kRows * i : -row0;    // (an address that exists: the first key's)
+        cp_async16_zfill(dst + at, kp + back * c.kst, n);
+        cp_async16_zfill(dst + Slice<D>::v_off + at, vp + back * c.vst, n);
+      }
+    }
+    // (16 keys from a multiple of 16 on lie in one block: one scale of K, one of V)
+    if ((lane & 15) == 0) cp_async4_zfill(dst + Slice<D>::scale_off + 4 * lane, sp + (int64_t)(key >> c.shift) * c.Hkv, 4u);
+  };
+  auto advance = [&]() {
+    if (in.next(c, a.pos, LY::chunk, heads)) {
+      aim(0);
+    } else {
+      kp += LY::chunk * c.kst;
+      vp += LY::chunk * c.vst;
+      key += LY::chunk;
     }
   };
+  aim(k0);
   // (a group is committed every time, so that "all but the newest STAGES - 1" always includes this chunk's)
-#pragma unroll
+#pragma unroll 1
   for (int s = 0; s < STAGES - 1; ++s) {
-    if (lo + s < hi) {
-      if (s) in.next(c, a.pos, LY::chunk, heads);
-      issue(in, s);
+    if (s < todo) {
+      if (s) advance();
+      issue(s);
     }
     cp_async_commit();
   }
   WS ws;
-  bool fresh = true;
-  int stage = 0, ahead = STAGES - 1, segment = 0;
-  for (int64_t at = lo; at < hi; ++at) {
-    if (at + STAGES - 1 < hi) {
-      if (STAGES > 1) in.next(c, a.pos, LY::chunk, heads);
-      issue(in, ahead);
+  int stage = 0, ahead = STAGES - 1, segment = 0, since = 0;  // `since`: chunks of the present (KV head, group) behind it
+  int h0 = 0, nh = 0;
+#pragma unroll 1
+  for (int it = 0; it < todo; ++it) {
+    if (it + STAGES - 1 < todo) {
+      advance();
+      issue(ahead);
     }
     cp_async_commit();
-    const int sub = cur.hg % a.NS, h0 = cur.hg / a.NS * a.G + sub * kGMaxGroup, nh = min(kGMaxGroup, a.G - sub * kGMaxGroup);
-    if (fresh) {
+    if (since == 0) {
+      const int sub = cur.hg % a.NS;
+      h0 = cur.hg / a.NS * a.G + sub * kGMaxGroup;
+      nh = min(kGMaxGroup, a.G - sub * kGMaxGroup);
       ws.reset();
       ws.load_q(reinterpret_cast<const T*>(a.q) + ((int64_t)cur.b * a.Hq + h0) * D, nh, a.scale_log2);
-      fresh = false;
     }
     cp_async_wait<STAGES - 1>();
     __syncwarp();
-    const int key0 = cur.k * LY::chunk + warp * kSlice;
-    if (key0 < cur.len) {
+    const uint32_t slice = ring + stage * Slice<D>::bytes;
+    if (cur.live >= kSlice) {
+      ws.template step<true, true>(slice, 15u);
+    } else if (cur.live > 0) {
       const int row = lane >> 2;
-      ws.step(ring + stage * Slice<D>::bytes, (key0 + row < cur.len ? 3u : 0u) | (key0 + row + 8 < cur.len ? 12u : 0u));
+      ws.template step<false, true>(slice, (row < cur.live ? 3u : 0u) | (row + 8 < cur.live ? 12u : 0u));
     }
     __syncwarp();                                            // the stage is free for the copy the next trip issues
     stage = stage + 1 == STAGES ? 0 : stage + 1;
     ahead = ahead + 1 == STAGES ? 0 : ahead + 1;
-    if (cur.k + 1 == cur.n || at + 1 == hi) {
+    ++since;
+    if (cur.left == 1 || it + 1 == todo) {
       // ---- the end of this block's share of (sequence, KV head, group): the warps meet
-      const bool whole = cur.k + 1 == cur.n && at - lo >= cur.n - 1;
+      const bool whole = cur.left == 1 && since == cur.n;
       ws.store(mg + warp * (kGMaxGroup * WS::kRow));
       __syncthreads();
       float* part = partial + (int64_t)(2 * blockIdx.x + (segment > 0)) * kPartial<D>;
@@ -486,9 +538,9 @@ cache_decode_kernel(CacheDecode a, DamCacheView c, float* __restrict__ partial) 
       }
       __syncthreads();                                       // before the next end overwrites the rows
       ++segment;
-      fresh = true;
+      since = 0;
     }
-    if (at + 1 < hi) cur.next(c, a.pos, LY::chunk, heads);
+    if (it + 1 < todo) cur.next(c, a.pos, LY::chunk, heads);
   }
 }
 
@@ -506,44 +558,30 @@ cache_join_kernel(CacheDecode a, DamCacheView c, const float* __restrict__ parti
   const int tid = threadIdx.x, lane = tid & 31, way = tid / TD, col = tid % TD;
   const int n = chunks_of(c, a.pos, b, chunk);
   if (g >= nh || n == 0) return;
-  int64_t sum = 0, before = 0;
+  int sum = 0, before = 0;
   for (int x = lane; x < c.num_seqs; x += 32) {
     const int m = chunks_of(c, a.pos, x, chunk);
     sum += m;
     before += x < b ? m : 0;
   }
-#pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
-    sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
-    before += __shfl_xor_sync(0xFFFFFFFFu, before, o);
-  }
-  const int64_t total = sum * heads, first = before * heads + (int64_t)hg * n, last = first + n - 1;
-  auto share_of = [&](int64_t at) -> int {
-    int s = (int)(at * shares / total);
-    while (s + 1 < shares && share_begin(total, s + 1, shares) <= at) ++s;
-    while (s > 0 && share_begin(total, s, shares) > at) --s;
-    return s;
-  };
-  const int s0 = share_of(first), s1 = share_of(last);
+  sum = __reduce_add_sync(0xFFFFFFFFu, sum);
+  before = __reduce_add_sync(0xFFFFFFFFu, before);
+  const Shares sh(sum * heads, shares);
+  const int first = before * heads + hg * n, last = first + n - 1;
+  const int s0 = sh.of(first), s1 = sh.of(last);
   if (s0 == s1) return;
   float mx = -CUDART_INF_F, lt = 0.f;
   float4 ot = make_float4(0.f, 0.f, 0.f, 0.f);
-  // (a share without a chunk lies between others when there are fewer chunks than shares; its range is empty)
-  auto row_of = [&](int s) -> const float* {
-    const int64_t lo = share_begin(total, s, shares);
-    if (lo == share_begin(total, s + 1, shares)) return nullptr;
-    return partial + (int64_t)(2 * s + (lo < first)) * kPartial<D>;
-  };
+  // (every share from s0 to s1 has chunks; where its first is an earlier (KV head, group)'s, this one's is its second result)
+  auto row_of = [&](int s) -> const float* { return partial + (int64_t)(2 * s + (sh.begin(s) < first)) * kPartial<D>; };
   for (int s = s0 + lane; s <= s1; s += 32) {
-    const float* r = row_of(s);
-    if (r) mx = fmaxf(mx, r[kGMaxGroup * D + g]);
+    mx = fmaxf(mx, row_of(s)[kGMaxGroup * D + g]);
   }
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xFFFFFFFFu, mx, o));
 #pragma unroll 4
   for (int s = s0 + way; s <= s1; s += WAYS) {
     const float* r = row_of(s);
-    if (!r) continue;
     const float f = weight(r[kGMaxGroup * D + g], mx);
     const float4 v = *reinterpret_cast<const float4*>(r + g * D + 4 * col);
     lt += r[kGMaxGroup * (D + 1) + g] * f;
@@ -665,7 +703,7 @@ cache_decode_masked_kernel(CacheDecode a, DamCacheView c, const unsigned char* _
           for (int e = 0; e < 2; ++e) keep |= (whs[(2 * quad + e) * kGRoundWords + (code >> 5)] >> (code & 31u) & 1u) << (2 * k + e);
         }
       }
-      ws.step(ring + it % kMStages * Slice<D>::bytes, keep);
+      ws.template step<false, false>(ring + it % kMStages * Slice<D>::bytes, keep);
       __syncwarp();                                          // the stage is free for the copy the next trip issues
     }
     cp_async_wait<0>();                                      // (only empty groups are left; the merge reuses the ring)
@@ -764,6 +802,7 @@ cudaError_t launch_dense(const CacheDecode& a, const DamCacheView& c, const dam_
     most += n * heads;
     longest = n > longest ? n : longest;
   }
+  if (most > 0x7FFFFFFF) return cudaErrorNotSupported;
   int shares = sms < kMaxShares ? sms : kMaxShares;
   if (most < shares) shares = most > 0 ? (int)most : 1;
   float* partial = reinterpret_cast<float*>(a.scratch + 64);
