@@ -6,12 +6,14 @@
 // Where the block of tokens was begun by an earlier call its scale can only grow, and when it does the tokens that are
 // there are read back and quantised again.  Read: value = code * scale.  Both move bytes and do little else: HBM bounds them
 // (2 + 1 bytes per element of a bf16 write, 1 + 2 of a read).
+#include <type_traits>
+
 #include "dam_cache.cuh"
 
 namespace {
 
 constexpr int kCThreads = 256;
-constexpr int kReadTokens = 64;        // packed tokens of a read's slot
+constexpr int kReadShift = 6, kReadTokens = 1 << kReadShift;   // packed tokens of a read's slot
 
 // 8 consecutive elements as they are in memory, and as fp32
 template <typename T> struct Eight;
@@ -24,10 +26,14 @@ template <> struct Eight<__nv_bfloat16> {
 #pragma unroll
     for (int i = 0; i < 4; ++i) { x[2 * i] = __uint_as_float(w[i] << 16); x[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u); }
   }
-  // largest magnitudes so far, two at a time: as bits, where an infinity or a NaN is larger than any number
+  // largest magnitudes so far, two at a time; as bits an infinity or a NaN is larger than any number
   __device__ __forceinline__ void top(uint32_t& t) const {
-    t = __vmaxu2(__vmaxu2(t, a.x & 0x7FFF7FFFu), a.y & 0x7FFF7FFFu);
-    t = __vmaxu2(__vmaxu2(t, a.z & 0x7FFF7FFFu), a.w & 0x7FFF7FFFu);
+    const uint32_t w[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const __nv_bfloat162 m = __hmax2_nan(*reinterpret_cast<const __nv_bfloat162*>(&t), __habs2(*reinterpret_cast<const __nv_bfloat162*>(&w[i])));
+      t = *reinterpret_cast<const uint32_t*>(&m);
+    }
   }
   static __device__ __forceinline__ uint32_t joined(uint32_t t) { return max(t << 16, t & 0xFFFF0000u); }
   static __device__ __forceinline__ void store(__nv_bfloat16* p, const float* x) {
@@ -67,17 +73,15 @@ __device__ __forceinline__ float block_scale(uint32_t top, bool begun, float bef
   if (!begun) return s;
   return s != s || before != before ? dam_cache_nan() : fmaxf(before, s);
 }
-// eight elements of a token that is there already, from the scale `before` to the scale s
+// eight elements of a token that is there already, from the scale `before` to the coder's
 template <int CODE>
-__device__ __forceinline__ void requantise(unsigned char* p, float before, float s, float inv) {
+__device__ __forceinline__ void requantise(unsigned char* p, float before, const Coder<CODE>& coder) {
   uint2* at = reinterpret_cast<uint2*>(p);
   const uint2 old = *at;
   float f[8];
-  codes_to_float<CODE>(old.x, f);
-  codes_to_float<CODE>(old.y, f + 4);
-#pragma unroll
-  for (int k = 0; k < 8; ++k) f[k] *= before;
-  *at = cache_codes8<CODE>(f, s, inv);
+  code_values<CODE>(old.x, before, f);
+  code_values<CODE>(old.y, before, f + 4);
+  *at = coder.eight(f);
 }
 
 // start of sequence b's range, and whether the range [start, start + n) lies inside its capacity (an empty one always does)
@@ -88,7 +92,7 @@ __device__ __forceinline__ bool range_fits(const DamCacheView& c, const int32_t*
 // the scratch block of the whole call, its status word included (one block of threads looks at every sequence)
 __device__ __forceinline__ void report_ranges(const DamCacheView& c, const int32_t* tok_cu, const int32_t* starts, uint32_t* scratch) {
   bool bad = false;
-  for (int b = threadIdx.x; b < c.num_seqs; b += kCThreads) {
+  for (int b = threadIdx.x; b < c.num_seqs; b += blockDim.x) {
     int start;
     bad |= !range_fits(c, starts, b, __ldg(tok_cu + b + 1) - __ldg(tok_cu + b), &start);
   }
@@ -102,64 +106,122 @@ struct CacheRows {               // K and V rows of the packed tokens
   const int32_t* cu;
 };
 
-// One (block of tokens, K or V, KV head) of a write.
-template <typename T>
-struct WriteUnit {
-  const T* x;                    // row of token `start`
-  unsigned char* codes;          // row of token 0
-  float* scale;
-  int64_t xst, cst;
-  int p0, lo, p1, start;         // the block's first token; its new tokens lo .. p1 - 1
-  // unit u of the grid's list: (slot, K or V, KV head), the head fastest.  False: nothing to do there.  (whole warp)
-  __device__ __forceinline__ bool find(const CacheRows& src, const int32_t* starts, const DamCacheView& c, uint32_t u) {
-    const int h = u % c.Hkv, kv = u / c.Hkv & 1;
-    const int64_t slot = u / (2 * c.Hkv);
-    const int b = cache_seq_of_slot(src.cu, c.num_seqs, c.shift, 2, slot);
-    const int t0 = __ldg(src.cu + b), n = __ldg(src.cu + b + 1) - t0, cap0 = __ldg(c.cu + b);
-    if (!range_fits(c, starts, b, n, &start) || n == 0) return false;
-    const int64_t j = (start >> c.shift) + (slot - ((t0 >> c.shift) + 2ll * b));
-    if (j > (start + n - 1) >> c.shift) return false;
-    p0 = (int)j << c.shift; p1 = min(p0 + (1 << c.shift), start + n); lo = max(p0, start);
-    xst = kv ? src.vst : src.kst; cst = kv ? c.vst : c.kst;
-    x = reinterpret_cast<const T*>(kv ? src.V : src.K) + (int64_t)t0 * xst + (int64_t)h * (kv ? src.vsh : src.ksh);
-    codes = (kv ? c.v : c.k) + (int64_t)cap0 * cst + (int64_t)h * (kv ? c.vsh : c.ksh);
-    scale = (kv ? c.vs : c.ks) + ((cap0 >> c.shift) + b + j) * c.Hkv + h;
-    return true;
+// A block of threads' way through the slots: its KV head and its side (K or V) stay, its slots are `step` apart, so that blocks
+// that run side by side read the heads of the same tokens (contiguous in memory).  SLOT finds a slot's tokens; its search of the
+// sequence runs only where the next slot is another sequence's (whole warp, the same in all warps).
+template <typename SLOT>
+struct Slots {
+  SLOT at;
+  uint32_t slot, until, step;    // until: first slot of the next sequence
+  int h, kv;
+  __device__ __forceinline__ Slots(const DamCacheView& c) : until(0) {
+    const uint32_t lane = blockIdx.x % (2 * c.Hkv);          // (the grid is a multiple of 2 Hkv)
+    kv = lane >= (uint32_t)c.Hkv;
+    h = (int)lane - (kv ? c.Hkv : 0);
+    slot = blockIdx.x / (2 * c.Hkv);
+    step = gridDim.x / (2 * c.Hkv);
+  }
+  // to the first slot from this one on that holds tokens
+  __device__ __forceinline__ bool seek(const DamCacheView& c, const CacheRows& rows, const int32_t* starts, uint32_t slots) {
+    for (; slot < slots; slot += step) {
+      if (slot >= until) until = at.enter(c, rows, starts, slot);
+      if (at.place(c, slot)) {
+        at.aim(c, rows, kv, h, step);
+        return true;
+      }
+    }
+    return false;
+  }
+  __device__ __forceinline__ bool next(const DamCacheView& c, const CacheRows& rows, const int32_t* starts, uint32_t slots) {
+    slot += step;
+    if (slot < until && at.place(c, slot)) {
+      at.go_on();
+      return true;
+    }
+    return seek(c, rows, starts, slots);
   }
 };
 
-// PASSES: rows of a block of tokens that a thread holds 8 elements of.  The blocks of threads stay and take one unit after
-// another; the rows of the next are on their way while this one's are quantised.
-template <typename T, int D, int CODE, int PASSES>
-__global__ void __launch_bounds__(kCThreads, PASSES * sizeof(T) <= 8 ? 5 : PASSES * sizeof(T) <= 16 ? 3 : 2)
-cache_write_kernel(CacheRows src, const int32_t* __restrict__ starts, DamCacheView c, uint32_t units, uint32_t* __restrict__ scratch) {
+// Slot of a write: one block of tokens of a sequence.  The pointers are a thread's own: row r0 of the block, element e.
+template <typename T, int D>
+struct WriteSlot {
+  int b, t0, cap0, start, end;   // sequence; its packed and its cache row; its new tokens start .. end - 1 (none: start == end)
+  int zero;                      // slot `x` is block x - zero of the sequence
+  const T* x;
+  unsigned char* codes;
+  float* scale;
+  int64_t xst, cst;
+  int64_t dx, dc, ds;            // to the next slot of the same sequence
+  int p0, first, last;           // the block's first token; its new tokens: rows first .. last - 1 of it
+  __device__ __forceinline__ uint32_t enter(const DamCacheView& c, const CacheRows& src, const int32_t* starts, uint32_t slot) {
+    b = cache_seq_of_slot(src.cu, c.num_seqs, c.shift, 2, slot);
+    t0 = __ldg(src.cu + b);
+    cap0 = __ldg(c.cu + b);
+    const int t1 = __ldg(src.cu + b + 1);
+    end = range_fits(c, starts, b, t1 - t0, &start) ? start + (t1 - t0) : start;
+    zero = (t0 >> c.shift) + 2 * b - (start >> c.shift);
+    return (uint32_t)(t1 >> c.shift) + 2u * (uint32_t)(b + 1);
+  }
+  __device__ __forceinline__ bool place(const DamCacheView& c, uint32_t slot) {
+    const int64_t p = ((int64_t)(int)slot - zero) << c.shift;
+    if (p >= end || start == end) return false;
+    p0 = (int)p;
+    first = max(start - p0, 0);
+    last = min(1 << c.shift, end - p0);
+    return true;
+  }
+  __device__ __forceinline__ void aim(const DamCacheView& c, const CacheRows& src, int kv, int h, uint32_t step) {
+    constexpr int TPR = D / 8;
+    const int r0 = threadIdx.x / TPR, e = threadIdx.x % TPR * 8;
+    xst = kv ? src.vst : src.kst; cst = kv ? c.vst : c.kst;
+    const int64_t tokens = (int64_t)step << c.shift;
+    dx = tokens * xst; dc = tokens * cst; ds = (int64_t)step * c.Hkv;
+    // (row t0 + p0 - start may lie before the sequence's where the block was begun before; it is not read then)
+    x = reinterpret_cast<const T*>(kv ? src.V : src.K) + ((int64_t)t0 + p0 - start + r0) * xst + (int64_t)h * (kv ? src.vsh : src.ksh) + e;
+    codes = (kv ? c.v : c.k) + ((int64_t)cap0 + p0 + r0) * cst + (int64_t)h * (kv ? c.vsh : c.ksh) + e;
+    scale = (kv ? c.vs : c.ks) + (int64_t)((cap0 >> c.shift) + b + (p0 >> c.shift)) * c.Hkv + h;
+  }
+  __device__ __forceinline__ void go_on() { x += dx; codes += dc; scale += ds; }
+};
+
+// PASSES: rows of a block of tokens that a thread holds 8 elements of.  The rows of the next slot are on their way while this
+// one's are quantised.
+template <typename T, int D, int CODE, int THREADS, int PASSES, int BLOCKS>
+__global__ void __launch_bounds__(THREADS, BLOCKS)
+cache_write_kernel(CacheRows src, const int32_t* __restrict__ starts, DamCacheView c, uint32_t slots, uint32_t* __restrict__ scratch) {
   dam_chain_prologue();
-  constexpr int TPR = D / 8, RPP = kCThreads / TPR;          // threads of a row, rows of a pass
-  __shared__ uint32_t warp_max[2][kCThreads / 32];
+  constexpr int TPR = D / 8, RPP = THREADS / TPR;            // threads of a row, rows of a pass
+  __shared__ uint32_t warp_max[2][THREADS / 32];
   if (blockIdx.x == 0) report_ranges(c, src.cu, starts, scratch);
-  const int tid = threadIdx.x, r0 = tid / TPR, e = tid % TPR * 8;
-  WriteUnit<T> cur, nxt;
+  const int tid = threadIdx.x, r0 = tid / TPR;
+  constexpr int whole = PASSES * RPP;                        // = block_tokens
+  Slots<WriteSlot<T, D>> it(c);
   Eight<T> v[PASSES], w[PASSES];
   float before = 0.f, before_next = 0.f;
-  auto load = [&](const WriteUnit<T>& y, Eight<T>* r, float& b) {
-    b = y.lo > y.p0 ? *reinterpret_cast<const volatile float*>(y.scale) : 0.f;
+  auto load = [&](const WriteSlot<T, D>& y, Eight<T>* r, float& b) {
+    if (y.first == 0 && y.last == whole) {
+#pragma unroll
+      for (int i = 0; i < PASSES; ++i) r[i].load(y.x + i * RPP * y.xst);
+      return;
+    }
+    b = y.first > 0 ? *reinterpret_cast<const volatile float*>(y.scale) : 0.f;
 #pragma unroll
     for (int i = 0; i < PASSES; ++i) {
-      const int p = y.p0 + r0 + i * RPP;
       r[i].clear();
-      if (p >= y.lo && p < y.p1) r[i].load(y.x + (int64_t)(p - y.start) * y.xst + e);
+      if (r0 + i * RPP >= y.first && r0 + i * RPP < y.last) r[i].load(y.x + i * RPP * y.xst);
     }
   };
-  uint32_t u = blockIdx.x;
-  bool have = false;
-  while (u < units && !(have = cur.find(src, starts, c, u))) u += gridDim.x;
-  if (have) load(cur, v, before);
+  bool have = it.seek(c, src, starts, slots);
+  if (have) load(it.at, v, before);
   int turn = 0;
   while (have) {
-    bool more = false;
-    u += gridDim.x;                                          // (units and the grid together stay below 2^32)
-    while (u < units && !(more = nxt.find(src, starts, c, u))) u += gridDim.x;
-    if (more) load(nxt, w, before_next);
+    // this slot's, while the cursor goes on
+    unsigned char* const codes = it.at.codes;
+    float* const scale = it.at.scale;
+    const int64_t cst = it.at.cst;
+    const int first = it.at.first, last = it.at.last;
+    have = it.next(c, src, starts, slots);
+    if (have) load(it.at, w, before_next);
     uint32_t top = 0u;
 #pragma unroll
     for (int i = 0; i < PASSES; ++i) v[i].top(top);
@@ -167,26 +229,39 @@ cache_write_kernel(CacheRows src, const int32_t* __restrict__ starts, DamCacheVi
     if ((tid & 31) == 0) warp_max[turn][tid >> 5] = top;
     __syncthreads();                                         // (every thread has read the old scale, too)
 #pragma unroll
-    for (int k = 0; k < kCThreads / 32; ++k) top = max(top, warp_max[turn][k]);
-    const float s = block_scale<CODE>(top, cur.lo > cur.p0, before);
-    const bool ok = s == s;
-    const float inv = ok ? 1.f / s : 0.f;
+    for (int k = 0; k < THREADS / 32; ++k) top = max(top, warp_max[turn][k]);
+    const float s = block_scale<CODE>(top, first > 0, before);
+    if (s == s) {
+      const Coder<CODE> coder(s);
+      if (first == 0 && last == whole) {
 #pragma unroll
-    for (int i = 0; i < PASSES; ++i) {
-      const int p = cur.p0 + r0 + i * RPP;
-      if (p >= cur.lo && p < cur.p1) {
-        float x[8];
-        v[i].floats(x);
-        *reinterpret_cast<uint2*>(cur.codes + (int64_t)p * cur.cst + e) = ok ? cache_codes8<CODE>(x, s, inv) : make_uint2(0u, 0u);
-      }
-    }
-    // where the scale grew the tokens that are there are read back and quantised again (every thread its own 8 elements)
-    if (cur.lo > cur.p0 && s > before) {
+        for (int i = 0; i < PASSES; ++i) {
+          float x[8];
+          v[i].floats(x);
+          *reinterpret_cast<uint2*>(codes + i * RPP * cst) = coder.eight(x);
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < PASSES; ++i) {
+          if (r0 + i * RPP >= first && r0 + i * RPP < last) {
+            float x[8];
+            v[i].floats(x);
+            *reinterpret_cast<uint2*>(codes + i * RPP * cst) = coder.eight(x);
+          }
+        }
+        // where the scale grew the tokens that are there are read back and quantised again (every thread its own 8 elements)
+        if (first > 0 && s > before) {
 #pragma unroll 1
-      for (int p = cur.p0 + r0; p < cur.lo; p += RPP) requantise<CODE>(cur.codes + (int64_t)p * cur.cst + e, before, s, inv);
+          for (int r = r0; r < first; r += RPP) requantise<CODE>(codes + (int64_t)(r - r0) * cst, before, coder);
+        }
+      }
+    } else {
+#pragma unroll 1
+      for (int r = r0; r < last; r += RPP)
+        if (r >= first) *reinterpret_cast<uint2*>(codes + (int64_t)(r - r0) * cst) = make_uint2(0u, 0u);
     }
-    if (tid == 0) *cur.scale = s;
-    cur = nxt; before = before_next; have = more; turn ^= 1;
+    if (tid == 0) *scale = s;
+    before = before_next; turn ^= 1;
 #pragma unroll
     for (int i = 0; i < PASSES; ++i) v[i] = w[i];
   }
@@ -195,19 +270,11 @@ cache_write_kernel(CacheRows src, const int32_t* __restrict__ starts, DamCacheVi
 // One token per sequence at most (a generation step): a warp per (sequence, K or V, KV head).
 template <typename T, int D, int CODE>
 __global__ void __launch_bounds__(128)
-cache_write_one_kernel(CacheRows src, const int32_t* __restrict__ starts, DamCacheView c, uint32_t units, uint32_t* __restrict__ scratch) {
+cache_write_one_kernel(CacheRows src, const int32_t* __restrict__ starts, DamCacheView c, uint32_t rows, uint32_t* __restrict__ scratch) {
   dam_chain_prologue();
-  if (blockIdx.x == 0) {
-    bool bad = false;
-    for (int b = threadIdx.x; b < c.num_seqs; b += 128) {
-      int start;
-      bad |= !range_fits(c, starts, b, __ldg(src.cu + b + 1) - __ldg(src.cu + b), &start);
-    }
-    const int st = __syncthreads_or(bad) ? (int)DAM_ERR_INVALID_ARGUMENT : 0;
-    if (threadIdx.x < 64) scratch[threadIdx.x] = threadIdx.x == 1 ? (uint32_t)st : 0u;
-  }
+  if (blockIdx.x == 0) report_ranges(c, src.cu, starts, scratch);
   const uint32_t u = blockIdx.x * 4 + (threadIdx.x >> 5);
-  if (u >= units) return;
+  if (u >= rows) return;
   constexpr int TPR = D / 8;
   const int lane = threadIdx.x & 31, r0 = lane / TPR, e = lane % TPR * 8;
   const int h = u % c.Hkv, kv = u / c.Hkv & 1, b = u / (2 * c.Hkv);
@@ -225,94 +292,103 @@ cache_write_one_kernel(CacheRows src, const int32_t* __restrict__ starts, DamCac
   v.top(top);
   top = __reduce_max_sync(0xFFFFFFFFu, Eight<T>::joined(top));
   const float s = block_scale<CODE>(top, start > p0, before);
-  const bool ok = s == s;
-  const float inv = ok ? 1.f / s : 0.f;
+  const Coder<CODE> coder(s);
   if (r0 == 0) {
     float x[8];
     v.floats(x);
-    *reinterpret_cast<uint2*>(codes + (int64_t)start * cst) = ok ? cache_codes8<CODE>(x, s, inv) : make_uint2(0u, 0u);
+    *reinterpret_cast<uint2*>(codes + (int64_t)start * cst) = s == s ? coder.eight(x) : make_uint2(0u, 0u);
   }
   if (start > p0 && s > before) {
 #pragma unroll 4
-    for (int p = p0 + r0; p < start; p += 32 / TPR) requantise<CODE>(codes + (int64_t)p * cst, before, s, inv);
+    for (int p = p0 + r0; p < start; p += 32 / TPR) requantise<CODE>(codes + (int64_t)p * cst, before, coder);
   }
   __syncwarp();                                              // (every lane has read the old scale)
   if (lane == 0) *scale = s;
 }
 
-// One (slot of kReadTokens packed tokens, K or V, KV head) of a read.
-template <typename T>
-struct ReadUnit {
-  T* x;                          // row of the slot's first token
+// Slot of a read: kReadTokens packed tokens of a sequence.  The pointers are a thread's own, as in WriteSlot.
+template <typename T, int D>
+struct ReadSlot {
+  int b, t0, cap0, start, all;   // sequence; its packed and its cache row; its tokens start .. start + all - 1
+  int zero;                      // slot `x` begins with token kReadTokens * (x - zero) of these
+  bool fits;
+  T* x;
   const unsigned char* codes;
   const float* scales;           // of block 0 of the sequence
   int64_t xst, cst;
-  int p, n;                      // the first token's place in its sequence; tokens left from it on (n < 0: to be zeros)
-  __device__ __forceinline__ bool find(const CacheRows& dst, const int32_t* starts, const DamCacheView& c, uint32_t u) {
-    constexpr int kShift = 6;
-    static_assert(1 << kShift == kReadTokens, "slots are counted by a shift");
-    const int h = u % c.Hkv, kv = u / c.Hkv & 1;
-    const int64_t slot = u / (2 * c.Hkv);
-    const int b = cache_seq_of_slot(dst.cu, c.num_seqs, kShift, 1, slot);
-    const int t0 = __ldg(dst.cu + b), all = __ldg(dst.cu + b + 1) - t0, cap0 = __ldg(c.cu + b);
-    int start;
-    const bool fits = range_fits(c, starts, b, all, &start);
-    const int64_t base = (slot - ((t0 >> kShift) + (int64_t)b)) * kReadTokens;
+  int64_t dx, dc;                // to the next slot of the same sequence
+  int row, p, n, readable;       // packed row and place of the slot's first token; tokens from it on; of those, how many can be read (n or none)
+  __device__ __forceinline__ uint32_t enter(const DamCacheView& c, const CacheRows& dst, const int32_t* starts, uint32_t slot) {
+    b = cache_seq_of_slot(dst.cu, c.num_seqs, kReadShift, 1, slot);
+    t0 = __ldg(dst.cu + b);
+    cap0 = __ldg(c.cu + b);
+    const int t1 = __ldg(dst.cu + b + 1);
+    all = t1 - t0;
+    fits = range_fits(c, starts, b, all, &start);
+    zero = (t0 >> kReadShift) + b;
+    return (uint32_t)(t1 >> kReadShift) + (uint32_t)(b + 1);
+  }
+  __device__ __forceinline__ bool place(const DamCacheView& c, uint32_t slot) {
+    const int64_t base = (int64_t)((int)slot - zero) << kReadShift;
     if (base >= all) return false;
     n = all - (int)base;
-    xst = kv ? dst.vst : dst.kst; cst = kv ? c.vst : c.kst;
-    x = reinterpret_cast<T*>(const_cast<void*>(kv ? dst.V : dst.K)) + (t0 + base) * xst + (int64_t)h * (kv ? dst.vsh : dst.ksh);
-    if (!fits) { n = -n; return true; }                      // nothing of this sequence can be read
-    p = start + (int)base;
-    codes = (kv ? c.v : c.k) + ((int64_t)cap0 + p) * cst + (int64_t)h * (kv ? c.vsh : c.ksh);
-    scales = (kv ? c.vs : c.ks) + (int64_t)((cap0 >> c.shift) + b) * c.Hkv + h;
+    readable = fits ? n : 0;
+    p = fits ? start + (int)base : 0;
+    row = t0 + (int)base;
     return true;
   }
+  __device__ __forceinline__ void aim(const DamCacheView& c, const CacheRows& dst, int kv, int h, uint32_t step) {
+    constexpr int TPR = D / 8;
+    const int r0 = threadIdx.x / TPR, e = threadIdx.x % TPR * 8;
+    xst = kv ? dst.vst : dst.kst; cst = kv ? c.vst : c.kst;
+    const int64_t tokens = (int64_t)step << kReadShift;
+    dx = tokens * xst; dc = tokens * cst;
+    x = reinterpret_cast<T*>(const_cast<void*>(kv ? dst.V : dst.K)) + ((int64_t)row + r0) * xst + (int64_t)h * (kv ? dst.vsh : dst.ksh) + e;
+    codes = (kv ? c.v : c.k) + ((int64_t)cap0 + p + r0) * cst + (int64_t)h * (kv ? c.vsh : c.ksh) + e;
+    scales = (kv ? c.vs : c.ks) + (int64_t)((cap0 >> c.shift) + b) * c.Hkv + h;
+  }
+  __device__ __forceinline__ void go_on() { x += dx; codes += dc; }
 };
 
+constexpr int kReadBlocks = 4;           // per SM
+
 template <typename T, int D, int CODE>
-__global__ void __launch_bounds__(kCThreads, 5)
-cache_read_kernel(CacheRows dst, const int32_t* __restrict__ starts, DamCacheView c, uint32_t units, uint32_t* __restrict__ scratch) {
+__global__ void __launch_bounds__(kCThreads, kReadBlocks)
+cache_read_kernel(CacheRows dst, const int32_t* __restrict__ starts, DamCacheView c, uint32_t slots, uint32_t* __restrict__ scratch) {
   dam_chain_prologue();
   constexpr int TPR = D / 8, RPP = kCThreads / TPR, PASSES = kReadTokens / RPP;
   if (blockIdx.x == 0) report_ranges(c, dst.cu, starts, scratch);
-  const int tid = threadIdx.x, r0 = tid / TPR, e = tid % TPR * 8;
-  ReadUnit<T> cur, nxt;
+  const int r0 = threadIdx.x / TPR;
+  Slots<ReadSlot<T, D>> it(c);
   uint2 v[PASSES], w[PASSES];
   float s[PASSES], z[PASSES];
-  auto load = [&](const ReadUnit<T>& y, uint2* r, float* f) {
+  auto load = [&](const ReadSlot<T, D>& y, uint2* r, float* f) {
 #pragma unroll
     for (int i = 0; i < PASSES; ++i) {
       const int t = r0 + i * RPP;
-      r[i] = make_uint2(0u, 0u);
+      r[i] = make_uint2(0u, 0u);                             // (a row that cannot be read: code 0 of scale 0)
       f[i] = 0.f;
-      if (t < y.n) {
-        r[i] = __ldcs(reinterpret_cast<const uint2*>(y.codes + (int64_t)t * y.cst + e));
+      if (t < y.readable) {
+        r[i] = __ldcs(reinterpret_cast<const uint2*>(y.codes + i * RPP * y.cst));
         f[i] = __ldg(y.scales + (int64_t)((y.p + t) >> c.shift) * c.Hkv);
       }
     }
   };
-  uint32_t u = blockIdx.x;
-  bool have = false;
-  while (u < units && !(have = cur.find(dst, starts, c, u))) u += gridDim.x;
-  if (have) load(cur, v, s);
+  bool have = it.seek(c, dst, starts, slots);
+  if (have) load(it.at, v, s);
   while (have) {
-    bool more = false;
-    u += gridDim.x;
-    while (u < units && !(more = nxt.find(dst, starts, c, u))) u += gridDim.x;
-    if (more) load(nxt, w, z);
+    T* const x = it.at.x;
+    const int64_t xst = it.at.xst;
+    const int n = it.at.n;
+    have = it.next(c, dst, starts, slots);
+    if (have) load(it.at, w, z);
 #pragma unroll
     for (int i = 0; i < PASSES; ++i) {
-      const int t = r0 + i * RPP;
       float f[8];
-      codes_to_float<CODE>(v[i].x, f);
-      codes_to_float<CODE>(v[i].y, f + 4);
-      // (the rows of a sequence that cannot be read become zeros: int8 code 0 of scale 0, or the e4m3 zero)
-#pragma unroll
-      for (int k = 0; k < 8; ++k) f[k] *= s[i];
-      if (t < abs(cur.n)) Eight<T>::store(cur.x + (int64_t)t * cur.xst + e, f);
+      code_values<CODE>(v[i].x, s[i], f);
+      code_values<CODE>(v[i].y, s[i], f + 4);
+      if (r0 + i * RPP < n) Eight<T>::store(x + i * RPP * xst, f);
     }
-    cur = nxt; have = more;
 #pragma unroll
     for (int i = 0; i < PASSES; ++i) { v[i] = w[i]; s[i] = z[i]; }
   }
@@ -322,35 +398,63 @@ CacheRows rows_of(const void* K, const void* V, const dam_shape_t* t) {
   return {K, V, t->k_stride_tok, t->k_stride_head, t->v_stride_tok, t->v_stride_head, t->cu_seqlens_dev};
 }
 
-template <typename T, int D, int CODE>
-cudaError_t launch_write(const CacheRows& src, const int32_t* starts, const DamCacheView& c, int64_t units, bool one, int sms, uint32_t* scratch,
-                         cudaStream_t st) {
-  if (one) {
-    return dam_launch_chained(cache_write_one_kernel<T, D, CODE>, dim3((unsigned)((units + 3) / 4)), dim3(128), 0, st, src, starts, c,
-                              (uint32_t)units, scratch);
+template <int N> using Int = std::integral_constant<int, N>;
+
+// Threads, rows per thread and blocks per SM of a write, by the elements of a block of tokens.
+template <typename T, int D, typename F>
+cudaError_t write_form(int block_tokens, F go) {
+  const int rows = block_tokens * (D / 64);                  // (of 64 elements)
+  if constexpr (sizeof(T) == 2) {
+    if (rows <= 16) return go(Int<128>(), Int<1>(), Int<8>());
+    if (rows == 32) return go(Int<128>(), Int<2>(), Int<8>());
+    if (rows == 64) return go(Int<128>(), Int<4>(), Int<6>());
+    if (rows == 128) return go(Int<128>(), Int<8>(), Int<4>());
+    if constexpr (D == 128) return go(Int<256>(), Int<8>(), Int<2>());
+  } else {
+    if (rows <= 16) return go(Int<128>(), Int<1>(), Int<8>());
+    if (rows == 32) return go(Int<128>(), Int<2>(), Int<6>());
+    if (rows == 64) return go(Int<128>(), Int<4>(), Int<4>());
+    if (rows == 128) return go(Int<256>(), Int<4>(), Int<2>());
+    if constexpr (D == 128) return go(Int<512>(), Int<4>(), Int<1>());
   }
-  const int passes = ((1 << c.shift) * (D / 8) + kCThreads - 1) / kCThreads;
-  void (*k)(CacheRows, const int32_t*, DamCacheView, uint32_t, uint32_t*) =
-      passes <= 1 ? cache_write_kernel<T, D, CODE, 1> : passes == 2 ? cache_write_kernel<T, D, CODE, 2>
-      : passes == 4 ? cache_write_kernel<T, D, CODE, 4> : cache_write_kernel<T, D, CODE, 8>;
-  const int per_sm = passes * (int)sizeof(T) <= 8 ? 5 : passes * (int)sizeof(T) <= 16 ? 3 : 2;
-  const int64_t grid = units < (int64_t)sms * per_sm ? units : (int64_t)sms * per_sm;
-  return dam_launch_chained(k, dim3((unsigned)grid), dim3(kCThreads), 0, st, src, starts, c, (uint32_t)units, scratch);
+  return cudaErrorNotSupported;
+}
+
+// Blocks of a grid over `slots` of c: a multiple of 2 Hkv, no more than are resident at once (or one slot at a time).
+unsigned slot_grid(int64_t slots, const DamCacheView& c, int resident) {
+  const int64_t per = 2ll * c.Hkv, at_once = resident / per > 0 ? resident / per : 1;
+  return (unsigned)(per * (slots < at_once ? slots : at_once));
 }
 
 template <typename T, int D, int CODE>
-cudaError_t launch_read(const CacheRows& dst, const int32_t* starts, const DamCacheView& c, int64_t units, int sms, uint32_t* scratch,
+cudaError_t launch_write(const CacheRows& src, const int32_t* starts, const DamCacheView& c, int64_t slots, bool one, int sms, uint32_t* scratch,
+                         cudaStream_t st) {
+  if (one) {
+    const int64_t rows = slots * 2 * c.Hkv;
+    return dam_launch_chained(cache_write_one_kernel<T, D, CODE>, dim3((unsigned)((rows + 3) / 4)), dim3(128), 0, st, src, starts, c,
+                              (uint32_t)rows, scratch);
+  }
+  // 8 rows per thread (fp32: 4) of blocks of 128 threads keep what a slot costs beside its rows small, and still leave 4 blocks per SM
+  auto go = [&](auto threads, auto passes, auto blocks) {
+    constexpr int THREADS = decltype(threads)::value, PASSES = decltype(passes)::value, BLOCKS = decltype(blocks)::value;
+    return dam_launch_chained(cache_write_kernel<T, D, CODE, THREADS, PASSES, BLOCKS>, dim3(slot_grid(slots, c, sms * BLOCKS)), dim3(THREADS),
+                              0, st, src, starts, c, (uint32_t)slots, scratch);
+  };
+  return write_form<T, D>(1 << c.shift, go);
+}
+
+template <typename T, int D, int CODE>
+cudaError_t launch_read(const CacheRows& dst, const int32_t* starts, const DamCacheView& c, int64_t slots, int sms, uint32_t* scratch,
                         cudaStream_t st) {
-  const int64_t grid = units < 5ll * sms ? units : 5ll * sms;
-  return dam_launch_chained(cache_read_kernel<T, D, CODE>, dim3((unsigned)grid), dim3(kCThreads), 0, st, dst, starts, c, (uint32_t)units,
-                            scratch);
+  return dam_launch_chained(cache_read_kernel<T, D, CODE>, dim3(slot_grid(slots, c, sms * kReadBlocks)), dim3(kCThreads), 0, st, dst, starts, c,
+                            (uint32_t)slots, scratch);
 }
 
 cudaError_t sm_count(int* sms) {
   int dev = 0;
   DamDeviceInfo di;
   const cudaError_t e = dam_current_device(&dev, &di);
-  *sms = di.sm_count;
+  *sms = e == cudaSuccess ? di.sm_count : 0;
   return e;
 }
 
@@ -362,12 +466,12 @@ cudaError_t dam_launch_cache_write(const void* K, const void* V, const dam_shape
   int sms = 0;
   const cudaError_t e = sm_count(&sms);
   if (e != cudaSuccess) return e;
-  // a sequence's tokens touch at most (n - 2) / block + 2 blocks: its slots are two more than the difference of cu / block
   bool one = true;
   for (int b = 0; b < c.num_seqs; ++b) one &= tokens->cu_seqlens_host[b + 1] - tokens->cu_seqlens_host[b] <= 1;
-  const int64_t slots = one ? c.num_seqs : (tokens->total_tokens >> c.shift) + 2ll * c.num_seqs, units = slots * 2 * c.Hkv;
-  if (units > 0x7FFFFFFF) return cudaErrorNotSupported;
-  return DAM_CACHE_DISPATCH(launch_write, tokens->dtype, tokens->head_dim, cache->code, rows_of(K, V, tokens), starts, c, units, one, sms,
+  // a sequence's tokens touch at most (n - 2) / block + 2 blocks: its slots are two more than the difference of cu / block
+  const int64_t slots = one ? c.num_seqs : (tokens->total_tokens >> c.shift) + 2ll * c.num_seqs;
+  if (slots * 2 * c.Hkv > 0x7FFFFFFF) return cudaErrorNotSupported;
+  return DAM_CACHE_DISPATCH(launch_write, tokens->dtype, tokens->head_dim, cache->code, rows_of(K, V, tokens), starts, c, slots, one, sms,
                             reinterpret_cast<uint32_t*>(scratch), st);
 }
 
@@ -377,8 +481,8 @@ cudaError_t dam_launch_cache_read(const dam_cache_t* cache, const dam_shape_t* t
   int sms = 0;
   const cudaError_t e = sm_count(&sms);
   if (e != cudaSuccess) return e;
-  const int64_t slots = tokens->total_tokens / kReadTokens + (int64_t)c.num_seqs, units = slots * 2 * c.Hkv;
-  if (units > 0x7FFFFFFF) return cudaErrorNotSupported;
-  return DAM_CACHE_DISPATCH(launch_read, tokens->dtype, tokens->head_dim, cache->code, rows_of(K, V, tokens), starts, c, units, sms,
+  const int64_t slots = tokens->total_tokens / kReadTokens + (int64_t)c.num_seqs;
+  if (slots * 2 * c.Hkv > 0x7FFFFFFF) return cudaErrorNotSupported;
+  return DAM_CACHE_DISPATCH(launch_read, tokens->dtype, tokens->head_dim, cache->code, rows_of(K, V, tokens), starts, c, slots, sms,
                             reinterpret_cast<uint32_t*>(scratch), st);
 }

@@ -40,22 +40,38 @@ __device__ __forceinline__ uint32_t biased_to_half2(uint32_t h) {
   asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(h), "r"(0x64806480u));
   return r;
 }
-// The four codes of a word as fp32 numbers.
+// Two fp32 numbers at a time.
+struct F2 {
+  uint64_t v;
+  __device__ __forceinline__ F2() {}
+  __device__ __forceinline__ F2(float x, float y) { asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "f"(x), "f"(y)); }
+  __device__ __forceinline__ void get(float& x, float& y) const { asm("mov.b64 {%0, %1}, %2;" : "=f"(x), "=f"(y) : "l"(v)); }
+};
+__device__ __forceinline__ F2 add2(F2 a, F2 b) { F2 r; asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v)); return r; }
+__device__ __forceinline__ F2 mul2(F2 a, F2 b) { F2 r; asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v)); return r; }
+__device__ __forceinline__ F2 fma2(F2 a, F2 b, F2 c) { F2 r; asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v)); return r; }
+
+// The values of the four codes of a word under the scale s.
 template <int CODE>
-__device__ __forceinline__ void codes_to_float(uint32_t w, float* f) {
+__device__ __forceinline__ void code_values(uint32_t w, float s, float* f) {
+  F2 lo, hi;
   if constexpr (CODE == DAM_CODE_INT8) {
     // 2^23 + 128 + c as fp32 bits, minus 2^23 + 128
     w ^= 0x80808080u;
+    uint32_t u[4];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) f[k] = __uint_as_float(__byte_perm(w, 0x4B000000u, 0x7440 | k)) - 8388736.f;
+    for (int k = 0; k < 4; ++k) u[k] = __byte_perm(w, 0x4B000000u, 0x7440 | k);
+    const F2 bias(-8388736.f, -8388736.f);
+    lo = add2(F2(__uint_as_float(u[0]), __uint_as_float(u[1])), bias);
+    hi = add2(F2(__uint_as_float(u[2]), __uint_as_float(u[3])), bias);
   } else {
-#pragma unroll
-    for (int k = 0; k < 2; ++k) {
-      const uint32_t h = e4m3x2_to_half2(w >> (16 * k));
-      const float2 v = __half22float2(*reinterpret_cast<const __half2*>(&h));
-      f[2 * k] = v.x; f[2 * k + 1] = v.y;
-    }
+    const uint32_t a = e4m3x2_to_half2(w & 0xFFFFu), b = e4m3x2_to_half2(w >> 16);
+    const float2 x = __half22float2(*reinterpret_cast<const __half2*>(&a)), y = __half22float2(*reinterpret_cast<const __half2*>(&b));
+    lo = F2(x.x, x.y); hi = F2(y.x, y.y);
   }
+  const F2 scale(s, s);
+  mul2(lo, scale).get(f[0], f[1]);
+  mul2(hi, scale).get(f[2], f[3]);
 }
 
 // ---- values -> codes ----------------------------------------------------------------------------
@@ -75,49 +91,73 @@ __device__ __forceinline__ float cache_scale(uint32_t amax) {
   }
 }
 
-// The codes of eight values under the scale s (inv = 1 / s).
+// What makes codes of values under one scale.
 template <int CODE>
-__device__ __forceinline__ uint2 cache_codes8(const float* x, float s, float inv) {
-  uint32_t w[2];
-  if constexpr (CODE == DAM_CODE_INT8) {
-    // The nearest integer to x / s, ties to even, decided on the exact quotient.  x * inv + 1.5 * 2^23 is rounded to an integer
-    // q (its low byte is the code); x * inv is off by 2^-16 at most, so q is right, or one off next to a border of two codes.
-    // There |x - q s| is s / 2 or next to it, and the difference is exact: a multiple of half an ulp of s.
-    constexpr float kMagic = 12582912.f;
-    float t[8], far = 0.f;
-#pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      t[k] = fmaf(x[k], inv, kMagic);
-      far = fmaxf(far, fabsf(fmaf(-(t[k] - kMagic), s, x[k])));
+struct Coder {
+  float s;
+  F2 lo, hi;                     // int8: 1 / s, a little less and a little more; e4m3: 1 / s
+  __device__ __forceinline__ explicit Coder(float scale) : s(scale) {
+    const float inv = 1.f / scale;
+    if constexpr (CODE == DAM_CODE_INT8) {
+      const float a = inv * (1.f - 2.3841858e-7f), b = inv * (1.f + 2.3841858e-7f);      // (2^-22)
+      lo = F2(a, a);
+      hi = F2(b, b);
+    } else {
+      lo = F2(inv, inv);
     }
-    const float half = 0.5f * s;
-    if (far >= half) {                 // (one of the eight, at most: few values are that near a border)
-#pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        const float q = t[k] - kMagic, r = fmaf(-q, s, x[k]);
-        const bool odd = (__float_as_uint(t[k]) & 1u) != 0;
-        if (r > half || (r == half && odd)) t[k] += 1.f;
-        else if (r < -half || (r == -half && odd)) t[k] -= 1.f;
-        t[k] = fminf(fmaxf(t[k], kMagic - 127.f), kMagic + 127.f);
-      }
-    }
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const uint32_t lo = __byte_perm(__float_as_uint(t[4 * i]), __float_as_uint(t[4 * i + 1]), 0x0040);
-      const uint32_t hi = __byte_perm(__float_as_uint(t[4 * i + 2]), __float_as_uint(t[4 * i + 3]), 0x0040);
-      w[i] = __byte_perm(lo, hi, 0x5410);
-    }
-  } else {
-    // (the scale is a power of two: x * inv is exact, or so small that its code is zero)
-    uint16_t h[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-      asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(h[i]) : "f"(x[2 * i + 1] * inv), "f"(x[2 * i] * inv));
-    w[0] = (uint32_t)h[0] | (uint32_t)h[1] << 16;
-    w[1] = (uint32_t)h[2] | (uint32_t)h[3] << 16;
   }
-  return make_uint2(w[0], w[1]);
-}
+  // The codes of eight values.
+  __device__ __forceinline__ uint2 eight(const float* x) const {
+    uint32_t w[2];
+    if constexpr (CODE == DAM_CODE_INT8) {
+      // The nearest integer to x / s, ties to even, of the exact quotient: x times a little less and a little more than 1 / s
+      // enclose it (1 / s and the two factors are off by 2^-23 together), so where both round to the same integer (the sum with
+      // 1.5 * 2^23 does that; its low byte is the code), the quotient does.  Otherwise x is next to a border of two codes.
+      constexpr float kMagic = 12582912.f;
+      const F2 magic(kMagic, kMagic);
+      float t[8];
+      uint32_t differ = 0u;
+#pragma unroll
+      for (int k = 0; k < 8; k += 2) {
+        const F2 v(x[k], x[k + 1]);
+        float a, b;
+        fma2(v, lo, magic).get(t[k], t[k + 1]);
+        fma2(v, hi, magic).get(a, b);
+        differ |= __float_as_uint(t[k]) ^ __float_as_uint(a);
+        differ |= __float_as_uint(t[k + 1]) ^ __float_as_uint(b);
+      }
+      if (differ) {                      // (of bf16 values: one that is an exact tie, or amax / 2)
+        // x - q s is s / 2 there, or next to it, and the difference is exact: a multiple of half an ulp of s
+        const float half = 0.5f * s;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          const float q = t[k] - kMagic, r = fmaf(-q, s, x[k]);
+          const bool odd = (__float_as_uint(t[k]) & 1u) != 0;
+          if (r > half || (r == half && odd)) t[k] += 1.f;
+          else if (r < -half || (r == -half && odd)) t[k] -= 1.f;
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const uint32_t a = __byte_perm(__float_as_uint(t[4 * i]), __float_as_uint(t[4 * i + 1]), 0x0040);
+        const uint32_t b = __byte_perm(__float_as_uint(t[4 * i + 2]), __float_as_uint(t[4 * i + 3]), 0x0040);
+        w[i] = __byte_perm(a, b, 0x5410);
+      }
+    } else {
+      // (the scale is a power of two: x / s is exact, or so small that its code is zero)
+      uint16_t h[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        float a, b;
+        mul2(F2(x[2 * i], x[2 * i + 1]), lo).get(a, b);
+        asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(h[i]) : "f"(b), "f"(a));
+      }
+      w[0] = (uint32_t)h[0] | (uint32_t)h[1] << 16;
+      w[1] = (uint32_t)h[2] | (uint32_t)h[3] << 16;
+    }
+    return make_uint2(w[0], w[1]);
+  }
+};
 
 // ---- which sequence -----------------------------------------------------------------------------
 // The work of a packed batch is cut into slots: sequence b owns the slots (cu[b] >> shift) + extra * b onwards, up to the next
