@@ -21,6 +21,7 @@
 
 #include "dam_cache.cuh"
 #include "dam_decode_common.cuh"
+#include "sm100_ptx.cuh"
 
 namespace {
 
@@ -69,18 +70,20 @@ __device__ __forceinline__ void codes_to_half(uint32_t w, uint32_t* h) {
   }
 }
 
-// Shared memory of one slice: 16 K rows, 16 V rows, 16 K scales, 16 V scales.  The 16-byte pieces of the rows are permuted so
-// that the eight lanes a 16-byte read is served for at a time find their pieces in different banks:
-//   head_dim 128: piece p of row r stands at p ^ (r & 7);
-//   head_dim 64:  two rows share 128 bytes; piece p of row r stands at ((r & 1) * 4 + p) ^ 2 * (r / 2 & 3) of them.
+// Rows of one slice in shared memory: 16 of K, 16 of V, as a tiled copy with 128-byte (head_dim 64: 64-byte) swizzle leaves them.
+// The 16-byte piece p of row r stands at piece p ^ (r & 7) of the row, for head_dim 64 at p ^ (r / 2 & 3): the eight lanes that a
+// 16-byte read is served for at a time find their pieces in different banks, given the order in which rows are taken.
 template <int D>
 struct Slice {
   static constexpr int pieces = D / 16;
-  static constexpr int v_off = kSlice * D, scale_off = 2 * kSlice * D, bytes = 2 * kSlice * D + 2 * kSlice * 4;
+  static constexpr int v_off = kSlice * D, bytes = 2 * kSlice * D;
   static __device__ __forceinline__ uint32_t at(int r, int p) {
     if constexpr (D == 128) return r * 128 + ((p ^ (r & 7)) << 4);
-    else return (r >> 1) * 128 + ((((r & 1) * 4 + p) ^ ((r >> 1 & 3) * 2)) << 4);
+    else return r * 64 + ((p ^ (r >> 1 & 3)) << 4);
   }
+  // The key that stands for row i of the instructions' tiles (i + 8: that key + 8).  head_dim 64: 0 3 4 7 1 2 5 6, so that rows 2 j
+  // and 2 j + 1 lie in different halves of 128 bytes (K), and rows 0 2 4 6, and 1 3 5 7, in different quarters (V).
+  static __device__ __forceinline__ int key(int i) { return D == 128 ? i : (int)(0x65217430u >> (4 * (i & 7)) & 7u) + (i & 8); }
 };
 
 // What a warp carries through the keys of one (sequence, up to 8 query heads of one KV head).  Lane = 4 row + quad: the lane
@@ -150,21 +153,27 @@ struct WarpState {
     qs[1] = __shfl_sync(0xFFFFFFFFu, back, 8 * quad + 4);
   }
 
-  // One slice.  ALL: every head keeps every key; otherwise keep: bit e (e + 2): head 2 quad + e keeps key row (row + 8); a key that
-  // a head does not keep has no part in it.  UNIFORM: the 16 keys share their scales (they lie in one block).
-  template <bool ALL, bool UNIFORM>
-  __device__ __forceinline__ void step(uint32_t slice, uint32_t keep) {
+  // One slice: rows at `slice`, scales at `sc`, and which keys there are for whom.
+  //   kAll    every head keeps all 16; they share their scales, K's and V's (they lie in one block)
+  //   kFirst  the same for the first `arg` of them; the rows behind may hold anything
+  //   kKeep   bit e (e + 2) of arg: head 2 quad + e keeps key `row` (key `row + 8`), keys by Slice::key; 16 scales of K and of V
+  // A key that a head does not keep has no part in it.
+  enum Mode { kAll, kFirst, kKeep };
+  template <Mode MODE>
+  __device__ __forceinline__ void step(uint32_t slice, uint32_t sc, uint32_t arg) {
     using SL = Slice<D>;
-    const int lane = threadIdx.x & 31, row = lane >> 2, quad = lane & 3;
-    const uint32_t sc = slice + SL::scale_off + (UNIFORM ? 0 : 4 * row);
-    const float ks0 = lds_float(sc), vs0 = lds_float(sc + 64);
-    const float ks1 = UNIFORM ? ks0 : lds_float(sc + 32), vs1 = UNIFORM ? vs0 : lds_float(sc + 96);
+    constexpr bool ALL = MODE == kAll, UNIFORM = MODE != kKeep;
+    const int lane = threadIdx.x & 31, row = lane >> 2, quad = lane & 3, key = SL::key(row);
+    uint32_t keep = arg;
+    if constexpr (MODE == kFirst) keep = (key < (int)arg ? 3u : 0u) | (key + 8 < (int)arg ? 12u : 0u);
+    const float ks0 = lds_float(sc + (UNIFORM ? 0 : 4 * key)), vs0 = lds_float(sc + (UNIFORM ? 4 : 64 + 4 * key));
+    const float ks1 = UNIFORM ? ks0 : lds_float(sc + 32 + 4 * key), vs1 = UNIFORM ? vs0 : lds_float(sc + 96 + 4 * key);
     auto kept = [&](int bit) { return ALL || (keep >> bit & 1u); };
     // S^T = K q^T: k-step s takes the dimensions D / 4 * quad + 4 s ... of a lane
     float st[2][4] = {};                                     // (two chains of instructions, half as long)
 #pragma unroll
     for (int c = 0; c < D / 64; ++c) {
-      const uint4 a = lds128(slice + SL::at(row, D / 64 * quad + c)), b = lds128(slice + SL::at(row + 8, D / 64 * quad + c));
+      const uint4 a = lds128(slice + SL::at(key, D / 64 * quad + c)), b = lds128(slice + SL::at(key + 8, D / 64 * quad + c));
       const uint32_t wa[4] = {a.x, a.y, a.z, a.w}, wb[4] = {b.x, b.y, b.z, b.w};
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
@@ -232,18 +241,22 @@ struct WarpState {
       pl0 = movmatrix_trans(pack_half2(w[0] - f0.x, w[1] - f0.y));
       pl1 = movmatrix_trans(pack_half2(w[2] - f1.x, w[3] - f1.y));
     }
-    // O^T += V^T P^T: the lane's rows are keys 2 quad, 2 quad + 1, 2 quad + 8, 2 quad + 9; their codes of one dimension are
-    // brought together byte by byte
+    // O^T += V^T P^T: the lane's rows are 2 quad, 2 quad + 1, 2 quad + 8, 2 quad + 9; their codes of one dimension are brought
+    // together byte by byte
     uint32_t vw[4][D / 32];
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
-      const int key = 2 * quad + (r & 1) + (r >> 1) * 8;
+      const int at = SL::key(2 * quad + (r & 1)) + (r >> 1) * 8;
       if constexpr (D == 128) {
-        const uint4 a = lds128(slice + SL::v_off + SL::at(key, row));
+        const uint4 a = lds128(slice + SL::v_off + SL::at(at, row));
         vw[r][0] = a.x; vw[r][1] = a.y; vw[r][2] = a.z; vw[r][3] = a.w;
       } else {
-        const uint2 a = lds64(slice + SL::v_off + SL::at(key, row >> 1) + (row & 1) * 8);
+        const uint2 a = lds64(slice + SL::v_off + SL::at(at, row >> 1) + (row & 1) * 8);
         vw[r][0] = a.x; vw[r][1] = a.y;
+      }
+      if constexpr (MODE == kFirst) {                        // (an e4m3 code behind the last key may be a NaN: 0 * NaN is not 0)
+#pragma unroll
+        for (int i = 0; i < D / 32; ++i) vw[r][i] = at < (int)arg ? vw[r][i] : 0u;
       }
     }
 #pragma unroll
@@ -280,15 +293,47 @@ struct WarpState {
       if (row == 0) { dst[D] = m[e]; dst[D + 1] = s; }
     }
   }
-  // dimension that stands at position p of a stored row
-  static __device__ __forceinline__ int dim_at(int p) { return D / 8 * ((p & 15) >> 1) + 2 * (p >> 4) + (p & 1); }
 };
 
 __device__ __forceinline__ void put(float* p, float v) { *p = v; }
 __device__ __forceinline__ void put(__nv_bfloat16* p, float v) { *p = __float2bfloat16_rn(v); }
+__device__ __forceinline__ void put2(float* p, float a, float b) { *reinterpret_cast<float2*>(p) = make_float2(a, b); }
+__device__ __forceinline__ void put2(__nv_bfloat16* p, float a, float b) { *reinterpret_cast<__nv_bfloat162*>(p) = __floats2bfloat162_rn(a, b); }
 __device__ __forceinline__ float lse_of(float m, float l) { return l == 0.f ? -CUDART_INF_F : (m + log2f(l)) * 0.6931471805599453f; }
 // weight of a partial result with reference m under the common reference mx (a partial result without a key has none)
 __device__ __forceinline__ float weight(float m, float mx) { return m == -CUDART_INF_F ? 0.f : g_ex2(m - mx); }
+
+// Four positions (p ... p + 3) of a row under a common reference.
+struct Fold {
+  float m, l;
+  float4 o;
+  // the rows of `n` warps, `stride` floats apart
+  template <int N>
+  __device__ __forceinline__ void warps(const float* row, int stride, int d, int p) {
+    m = -CUDART_INF_F; l = 0.f;
+    o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+    for (int w = 0; w < N; ++w) m = fmaxf(m, row[w * stride + d]);
+#pragma unroll
+    for (int w = 0; w < N; ++w) {
+      const float f = weight(row[w * stride + d], m);
+      add(f, row[w * stride + d + 1], *reinterpret_cast<const float4*>(row + w * stride + p));
+    }
+  }
+  __device__ __forceinline__ void add(float f, float sum, float4 x) {
+    l += sum * f;
+    o.x += x.x * f; o.y += x.y * f; o.z += x.z * f; o.w += x.w * f;
+  }
+  // the result: dimension D / 8 * row + 2 u + (0, 1) stands at position 16 u + 2 row + (0, 1)
+  template <int D, typename T>
+  __device__ __forceinline__ void write(T* O, float* lse, int p) const {
+    const float inv = l == 0.f ? 0.f : 1.f / l;              // (no key: O is zero already; a NaN stays one)
+    const int at = D / 8 * ((p & 15) >> 1) + 2 * (p >> 4);
+    put2(O + at, o.x * inv, o.y * inv);
+    put2(O + at + D / 8, o.z * inv, o.w * inv);
+    if (p == 0) *lse = lse_of(m, l);
+  }
+};
 
 struct CacheDecode {
   const void* q;
@@ -298,25 +343,38 @@ struct CacheDecode {
   void* O;
   float* lse;
   uint32_t* scratch;
+  int side;                    // see the next section
 };
 
 // ---- every key ----------------------------------------------------------------------------------
-// The keys of all (sequence, KV head, group of 8 heads) form one list of chunks (WARPS slices: one per warp), in that order; block
-// c of G takes the chunks [total c / G, total (c + 1) / G): every SM reads the same number of bytes, however ragged the batch.
-// Where a block's share ends inside a sequence's keys it leaves a partial result, and a second kernel joins those.
+// The keys of all sequences form one list of chunks (WARPS slices: one per warp), and share s of S takes the chunks [total s / S,
+// total (s + 1) / S): every SM reads the same number of bytes, however ragged the batch.  side > 1: that many (KV head, group of 8
+// heads), all of them, are served side by side, a block for each in every share: the rows that neighbouring blocks read at about the
+// same time are neighbours in memory.  side == 1: the list goes through the (KV head, group) of each sequence one after the other.
+// Where a share ends inside a sequence's keys it leaves a partial result, and a second kernel joins those.
 constexpr int kMaxShares = 148;        // blocks: one per SM of a B200
 
 __device__ __forceinline__ int chunks_of(const DamCacheView& c, const int32_t* pos, int b, int chunk) {
-  const int p = __ldg(pos + b);
-  return p < 0 || p >= __ldg(c.cu + b + 1) - __ldg(c.cu + b) ? 0 : p / chunk + 1;
+  const int p = __ldg(pos + b), room = __ldg(c.cu + b + 1) - __ldg(c.cu + b);
+  return (unsigned)p >= (unsigned)room ? 0 : p / chunk + 1;
 }
 
-// Chunks per head over all sequences (whole warp).
-__device__ __forceinline__ int total_chunks(const DamCacheView& c, const int32_t* pos, int chunk) {
-  int sum = 0;
-  for (int b = threadIdx.x & 31; b < c.num_seqs; b += 32) sum += chunks_of(c, pos, b, chunk);
-  return __reduce_add_sync(0xFFFFFFFFu, sum);
-}
+// Chunks per head of all sequences, of those before sequence b, and whether some position lies outside its capacity (whole warp).
+struct Survey {
+  int total, before;
+  bool bad;
+  __device__ __forceinline__ Survey(const DamCacheView& c, const int32_t* pos, int chunk, int b) : total(0), before(0), bad(false) {
+    for (int base = 0; base < c.num_seqs; base += 32) {
+      const int x = base + (threadIdx.x & 31);
+      const int n = x < c.num_seqs ? chunks_of(c, pos, x, chunk) : -1;
+      bad |= __any_sync(0xFFFFFFFFu, n == 0);
+      total += max(n, 0);
+      before += x < b ? max(n, 0) : 0;
+    }
+    total = __reduce_add_sync(0xFFFFFFFFu, total);
+    before = __reduce_add_sync(0xFFFFFFFFu, before);
+  }
+};
 
 // A place in the list of chunks.  Consumers and the copies that run ahead of them walk the list each on their own.
 struct Place {
@@ -336,7 +394,7 @@ struct Place {
     const int lane = threadIdx.x & 31;
     int before = 0;
     for (int base = 0; base < c.num_seqs; base += 32) {
-      const int mine = base + lane < c.num_seqs ? chunks_of(c, pos, base + lane, chunk) : 0;
+      const int mine = base + lane < c.num_seqs ? chunks_of(c, pos, base + lane, chunk) : 0;   // (read before: in the L1 cache)
       int incl = mine;
 #pragma unroll
       for (int o = 1; o < 32; o <<= 1) {
@@ -377,7 +435,11 @@ template <int D, int WARPS, int STAGES>
 struct DenseLayout {
   static constexpr int chunk = WARPS * kSlice;
   static constexpr int ring = WARPS * STAGES * Slice<D>::bytes;
-  static constexpr int total = ring + WARPS * kGMaxGroup * (D + 4) * 4;
+  static constexpr int merge_off = ring, merge = WARPS * kGMaxGroup * (D + 4) * 4;
+  static constexpr int scale_off = merge_off + merge;                           // [warp][stage] K scale, V scale
+  static constexpr int bar_off = scale_off + WARPS * STAGES * 8;                // [warp][stage]
+  static constexpr int flag_off = bar_off + WARPS * STAGES * 8;
+  static constexpr int total = flag_off + 16 + 1024;                            // (the ring starts on a multiple of 1024)
 };
 // floats of one partial result: O of 8 heads, references, sums
 template <int D> constexpr int kPartial = kGMaxGroup * (D + 2);
@@ -395,81 +457,79 @@ struct Shares {
 
 template <typename T, int D, int CODE, int WARPS, int STAGES>
 __global__ void __launch_bounds__(WARPS * 32, 1)
-cache_decode_kernel(CacheDecode a, DamCacheView c, float* __restrict__ partial) {
-  dam_chain_prologue();
+cache_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUtensorMap vmap, CacheDecode a, DamCacheView c,
+                    float* __restrict__ partial) {
   using LY = DenseLayout<D, WARPS, STAGES>;
   using WS = WarpState<T, D, CODE>;
-  extern __shared__ __align__(128) unsigned char sm[];
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, shares = gridDim.x, heads = c.Hkv * a.NS;
-  float* mg = reinterpret_cast<float*>(sm + LY::ring);
-  const uint32_t ring = static_cast<uint32_t>(__cvta_generic_to_shared(sm)) + warp * (STAGES * Slice<D>::bytes);
+  extern __shared__ unsigned char sm_raw[];
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int heads = a.side > 1 ? 1 : c.Hkv * a.NS;            // of the list
+  const int share = blockIdx.x / a.side, beside = blockIdx.x - share * a.side;
+  unsigned char* sm = sm_raw + (-sm100::smem_u32(sm_raw) & 1023u);
+  float* mg = reinterpret_cast<float*>(sm + LY::merge_off);
+  const uint32_t base = sm100::smem_u32(sm), ring = base + warp * (STAGES * Slice<D>::bytes);
+  const uint32_t scales = base + LY::scale_off + warp * (STAGES * 8), bars = base + LY::bar_off + warp * (STAGES * 8);
+  volatile uint32_t* const gave_up = reinterpret_cast<uint32_t*>(sm + LY::flag_off);
+  if (lane < STAGES) sm100::mbar_init(bars + 8 * lane, 1);
+  if (tid == 0) {
+    *gave_up = 0u;
+    sm100::tma_prefetch_desc(&kmap);
+    sm100::tma_prefetch_desc(&vmap);
+  }
+  sm100::mbar_fence_init();
+  __syncthreads();
+  // The joining kernel may begin when this one has seen its predecessors' memory: it reads the positions before it waits for this.
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  asm volatile("griddepcontrol.launch_dependents;");
+  const Survey all(c, a.pos, LY::chunk, 0);
   // sequences whose position lies outside their capacity get zeros; block 0 says so in the status word
-  bool any = false;
-  for (int b = tid; b < c.num_seqs; b += WARPS * 32) any |= chunks_of(c, a.pos, b, LY::chunk) == 0;
-  any = __syncthreads_or(any);
-  if (blockIdx.x == 0 && tid < 64) a.scratch[tid] = tid == 1 && any ? (uint32_t)DAM_ERR_INVALID_ARGUMENT : 0u;
-  if (any) {
-    for (int b = blockIdx.x; b < c.num_seqs; b += shares) {
+  if (blockIdx.x == 0 && tid < 64) a.scratch[tid] = tid == 1 && all.bad ? (uint32_t)DAM_ERR_INVALID_ARGUMENT : 0u;
+  if (all.bad) {
+    for (int b = blockIdx.x; b < c.num_seqs; b += gridDim.x) {
       if (chunks_of(c, a.pos, b, LY::chunk)) continue;
       for (int t = tid; t < a.Hq * D; t += WARPS * 32) put(reinterpret_cast<T*>(a.O) + (int64_t)b * a.Hq * D + t, 0.f);
       for (int t = tid; t < a.Hq; t += WARPS * 32) a.lse[(int64_t)b * a.Hq + t] = -CUDART_INF_F;
     }
   }
-  const Shares sh(total_chunks(c, a.pos, LY::chunk) * heads, shares);
-  const int lo = sh.begin(blockIdx.x), todo = sh.begin(blockIdx.x + 1) - lo;
+  const Shares sh(all.total * heads, gridDim.x / a.side);
+  const int lo = sh.begin(share), todo = sh.begin(share + 1) - lo;
   if (todo == 0) return;
   Place in, cur;
-  const int k0 = in.locate(c, a.pos, LY::chunk, heads, lo);
+  int key = in.locate(c, a.pos, LY::chunk, heads, lo) * LY::chunk + warp * kSlice;     // first key of the slice to be copied
   cur = in;
 
-  // The copies: this lane's 16-byte pieces of the slice's rows (rows lane / pieces + kRows i), and one scale (K's: lanes 0 .. 15).
-  constexpr int P = Slice<D>::pieces, kRows = 32 / P, kCopies = kSlice / kRows;
-  const int row0 = lane / P, piece = lane % P;
-  const unsigned char *kp, *vp;
+  // The copies: a tile of 16 rows of K, one of V, and their two scales (lanes 0 and 16).
   const float* sp;                     // scale of block 0 of the sequence
-  int key;                             // first key of the slice
-  auto aim = [&](int k) {
-    const int kvh = in.hg / a.NS;
-    const int64_t cu = __ldg(c.cu + in.b);
-    key = k * LY::chunk + warp * kSlice;
-    kp = c.k + (cu + key + row0) * c.kst + (int64_t)kvh * c.ksh + piece * 16;
-    vp = c.v + (cu + key + row0) * c.vst + (int64_t)kvh * c.vsh + piece * 16;
-    sp = (lane < 16 ? c.ks : c.vs) + ((cu >> c.shift) + in.b) * c.Hkv + kvh;
+  int kvh, token;                      // KV head; packed row of the slice's first key
+  auto aim = [&]() {
+    kvh = (in.hg + beside) / a.NS;
+    const int cu = __ldg(c.cu + in.b);
+    token = cu + key;
+    sp = (lane < 16 ? c.ks : c.vs) + (int64_t)((cu >> c.shift) + in.b) * c.Hkv + kvh;
   };
   auto issue = [&](int stage) {
     if (in.live <= 0) return;
-    const uint32_t dst = ring + stage * Slice<D>::bytes;
-    if (in.live >= kSlice) {
-#pragma unroll
-      for (int i = 0; i < kCopies; ++i) {
-        const uint32_t at = Slice<D>::at(row0 + kRows * i, piece);
-        cp_async16_zfill(dst + at, kp + i * kRows * c.kst, 16u);
-        cp_async16_zfill(dst + Slice<D>::v_off + at, vp + i * kRows * c.vst, 16u);
-      }
-    } else {                           // rows of keys that do not exist are filled with zeros
-#pragma unroll 1
-      for (int i = 0; i < kCopies; ++i) {
-        const int r = row0 + kRows * i;
-        const uint32_t n = r < in.live ? 16u : 0u, at = Slice<D>::at(r, piece);
-        const int back = r < in.live ? kRows * i : -row0;    // (an address that exists: the first key's)
-        cp_async16_zfill(dst + at, kp + back * c.kst, n);
-        cp_async16_zfill(dst + Slice<D>::v_off + at, vp + back * c.vst, n);
-      }
+    // (16 keys from a multiple of 16 on lie in one block.  A tile may reach into the rows behind the last key, of this sequence
+    // or of the next; rows beyond the cache read as zeros)
+    if ((lane & 15) == 0) cp_async4_zfill(scales + 8 * stage + (lane >> 2), sp + (int64_t)(key >> c.shift) * c.Hkv, 4u);
+    if (sm100::elect_one()) {
+      const uint32_t dst = ring + stage * Slice<D>::bytes, bar = bars + 8 * stage;
+      sm100::mbar_arrive_expect_tx(bar, Slice<D>::bytes);
+      sm100::tma_load_3d(dst, &kmap, bar, 0, kvh, token);
+      sm100::tma_load_3d(dst + Slice<D>::v_off, &vmap, bar, 0, kvh, token);
     }
-    // (16 keys from a multiple of 16 on lie in one block: one scale of K, one of V)
-    if ((lane & 15) == 0) cp_async4_zfill(dst + Slice<D>::scale_off + 4 * lane, sp + (int64_t)(key >> c.shift) * c.Hkv, 4u);
   };
   auto advance = [&]() {
     if (in.next(c, a.pos, LY::chunk, heads)) {
-      aim(0);
+      key = warp * kSlice;
+      aim();
     } else {
-      kp += LY::chunk * c.kst;
-      vp += LY::chunk * c.vst;
+      token += LY::chunk;
       key += LY::chunk;
     }
   };
-  aim(k0);
-  // (a group is committed every time, so that "all but the newest STAGES - 1" always includes this chunk's)
+  aim();
+  // (a group is committed every time, so that "all but the newest STAGES - 1" always includes this chunk's scales)
 #pragma unroll 1
   for (int s = 0; s < STAGES - 1; ++s) {
     if (s < todo) {
@@ -481,6 +541,8 @@ cache_decode_kernel(CacheDecode a, DamCacheView c, float* __restrict__ partial) 
   WS ws;
   int stage = 0, ahead = STAGES - 1, segment = 0, since = 0;  // `since`: chunks of the present (KV head, group) behind it
   int h0 = 0, nh = 0;
+  uint32_t phases = 0u;                // bit s: parity of the next copy into stage s
+  bool lost = false;                   // a copy did not arrive
 #pragma unroll 1
   for (int it = 0; it < todo; ++it) {
     if (it + STAGES - 1 < todo) {
@@ -489,20 +551,20 @@ cache_decode_kernel(CacheDecode a, DamCacheView c, float* __restrict__ partial) 
     }
     cp_async_commit();
     if (since == 0) {
-      const int sub = cur.hg % a.NS;
-      h0 = cur.hg / a.NS * a.G + sub * kGMaxGroup;
+      const int kv = (cur.hg + beside) / a.NS, sub = cur.hg + beside - kv * a.NS;
+      h0 = kv * a.G + sub * kGMaxGroup;
       nh = min(kGMaxGroup, a.G - sub * kGMaxGroup);
       ws.reset();
       ws.load_q(reinterpret_cast<const T*>(a.q) + ((int64_t)cur.b * a.Hq + h0) * D, nh, a.scale_log2);
     }
     cp_async_wait<STAGES - 1>();
     __syncwarp();
-    const uint32_t slice = ring + stage * Slice<D>::bytes;
-    if (cur.live >= kSlice) {
-      ws.template step<true, true>(slice, 15u);
-    } else if (cur.live > 0) {
-      const int row = lane >> 2;
-      ws.template step<false, true>(slice, (row < cur.live ? 3u : 0u) | (row + 8 < cur.live ? 12u : 0u));
+    if (cur.live > 0 && !lost) {
+      lost = !sm100::mbar_wait(bars + 8 * stage, phases >> stage & 1u, gave_up);
+      phases ^= 1u << stage;
+      const uint32_t slice = ring + stage * Slice<D>::bytes, sc = scales + 8 * stage;
+      if (cur.live >= kSlice) ws.template step<WS::kAll>(slice, sc, 15u);
+      else ws.template step<WS::kFirst>(slice, sc, (uint32_t)cur.live);
     }
     __syncwarp();                                            // the stage is free for the copy the next trip issues
     stage = stage + 1 == STAGES ? 0 : stage + 1;
@@ -514,26 +576,16 @@ cache_decode_kernel(CacheDecode a, DamCacheView c, float* __restrict__ partial) 
       ws.store(mg + warp * (kGMaxGroup * WS::kRow));
       __syncthreads();
       float* part = partial + (int64_t)(2 * blockIdx.x + (segment > 0)) * kPartial<D>;
-      for (int e = tid; e < nh * D; e += WARPS * 32) {
+      for (int e = 4 * tid; e < nh * D; e += WARPS * 128) {
         const int g = e / D, p = e % D;
-        const float* src = mg + g * WS::kRow;
-        float mx = -CUDART_INF_F, lt = 0.f, ot = 0.f;
-#pragma unroll
-        for (int w = 0; w < WARPS; ++w) mx = fmaxf(mx, src[w * (kGMaxGroup * WS::kRow) + D]);
-#pragma unroll
-        for (int w = 0; w < WARPS; ++w) {
-          const float* sw = src + w * (kGMaxGroup * WS::kRow);
-          const float f = weight(sw[D], mx);
-          lt += sw[D + 1] * f;
-          ot += sw[p] * f;
-        }
+        Fold f;
+        f.template warps<WARPS>(mg + g * WS::kRow, kGMaxGroup * WS::kRow, D, p);
         if (whole) {
           const int64_t h = (int64_t)cur.b * a.Hq + h0 + g;
-          put(reinterpret_cast<T*>(a.O) + h * D + WS::dim_at(p), lt == 0.f ? 0.f : ot / lt);
-          if (p == 0) a.lse[h] = lse_of(mx, lt);
+          f.template write<D>(reinterpret_cast<T*>(a.O) + h * D, a.lse + h, p);
         } else {
-          part[e] = ot;
-          if (p == 0) { part[kGMaxGroup * D + g] = mx; part[kGMaxGroup * (D + 1) + g] = lt; }
+          *reinterpret_cast<float4*>(part + e) = f.o;
+          if (p == 0) { part[kGMaxGroup * D + g] = f.m; part[kGMaxGroup * (D + 1) + g] = f.l; }
         }
       }
       __syncthreads();                                       // before the next end overwrites the rows
@@ -542,6 +594,7 @@ cache_decode_kernel(CacheDecode a, DamCacheView c, float* __restrict__ partial) 
     }
     if (it + 1 < todo) cur.next(c, a.pos, LY::chunk, heads);
   }
+  sm100::report_expired_wait(gave_up, a.scratch + 1, (uint32_t)DAM_ERR_DEVICE_TIMEOUT);
 }
 
 // Joins the partial results of one (sequence, KV head, group) and head; nothing to do where one block had all its keys.
@@ -549,55 +602,46 @@ cache_decode_kernel(CacheDecode a, DamCacheView c, float* __restrict__ partial) 
 template <typename T, int D>
 __global__ void __launch_bounds__(256)
 cache_join_kernel(CacheDecode a, DamCacheView c, const float* __restrict__ partial, int chunk, int shares) {
-  dam_chain_prologue();
-  constexpr int TD = D / 4, WAYS = 256 / TD;                 // threads of a row (4 dimensions each), partial results at a time
-  __shared__ float red[WAYS][D];
+  constexpr int TD = D / 4, WAYS = 256 / TD;                 // threads of a row (4 positions each), partial results at a time
+  __shared__ float4 red[WAYS][TD];
+  __shared__ float sums[WAYS];
+  // (before the wait: the positions, which the kernel before this one has read behind its own wait; it writes none)
+  asm volatile("griddepcontrol.launch_dependents;");
   const int heads = c.Hkv * a.NS, per = min(a.G, kGMaxGroup);
   const int g = blockIdx.x % per, hg = blockIdx.x / per % heads, b = blockIdx.x / per / heads;
   const int sub = hg % a.NS, nh = min(kGMaxGroup, a.G - sub * kGMaxGroup);
   const int tid = threadIdx.x, lane = tid & 31, way = tid / TD, col = tid % TD;
   const int n = chunks_of(c, a.pos, b, chunk);
-  if (g >= nh || n == 0) return;
-  int sum = 0, before = 0;
-  for (int x = lane; x < c.num_seqs; x += 32) {
-    const int m = chunks_of(c, a.pos, x, chunk);
-    sum += m;
-    before += x < b ? m : 0;
-  }
-  sum = __reduce_add_sync(0xFFFFFFFFu, sum);
-  before = __reduce_add_sync(0xFFFFFFFFu, before);
-  const Shares sh(sum * heads, shares);
-  const int first = before * heads + hg * n, last = first + n - 1;
-  const int s0 = sh.of(first), s1 = sh.of(last);
-  if (s0 == s1) return;
-  float mx = -CUDART_INF_F, lt = 0.f;
-  float4 ot = make_float4(0.f, 0.f, 0.f, 0.f);
+  const Survey all(c, a.pos, chunk, b);
+  const int list = a.side > 1 ? 1 : heads;
+  const Shares sh(max(all.total * list, 1), shares);
+  const int first = all.before * list + (a.side > 1 ? 0 : hg * n), s0 = sh.of(first), s1 = n ? sh.of(first + n - 1) : s0;
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  if (g >= nh || n == 0 || s0 == s1) return;
   // (every share from s0 to s1 has chunks; where its first is an earlier (KV head, group)'s, this one's is its second result)
-  auto row_of = [&](int s) -> const float* { return partial + (int64_t)(2 * s + (sh.begin(s) < first)) * kPartial<D>; };
-  for (int s = s0 + lane; s <= s1; s += 32) {
-    mx = fmaxf(mx, row_of(s)[kGMaxGroup * D + g]);
-  }
+  auto row_of = [&](int s) -> const float* { 
+    const int block = a.side > 1 ? s * a.side + hg : s;
+    return partial + (int64_t)(2 * block + (sh.begin(s) < first)) * kPartial<D>;
+  };
+  Fold f;
+  f.m = -CUDART_INF_F; f.l = 0.f;
+  f.o = make_float4(0.f, 0.f, 0.f, 0.f);
+  for (int s = s0 + lane; s <= s1; s += 32) f.m = fmaxf(f.m, row_of(s)[kGMaxGroup * D + g]);
 #pragma unroll
-  for (int o = 1; o < 32; o <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xFFFFFFFFu, mx, o));
+  for (int o = 1; o < 32; o <<= 1) f.m = fmaxf(f.m, __shfl_xor_sync(0xFFFFFFFFu, f.m, o));
 #pragma unroll 4
   for (int s = s0 + way; s <= s1; s += WAYS) {
     const float* r = row_of(s);
-    const float f = weight(r[kGMaxGroup * D + g], mx);
-    const float4 v = *reinterpret_cast<const float4*>(r + g * D + 4 * col);
-    lt += r[kGMaxGroup * (D + 1) + g] * f;
-    ot.x += v.x * f; ot.y += v.y * f; ot.z += v.z * f; ot.w += v.w * f;
+    f.add(weight(r[kGMaxGroup * D + g], f.m), r[kGMaxGroup * (D + 1) + g], *reinterpret_cast<const float4*>(r + g * D + 4 * col));
   }
-  __shared__ float sums[WAYS];
-  *reinterpret_cast<float4*>(&red[way][4 * col]) = ot;
-  if (col == 0) sums[way] = lt;
+  red[way][col] = f.o;
+  if (col == 0) sums[way] = f.l;
   __syncthreads();
-  if (tid < D) {
-    float o = 0.f, l = 0.f;
+  if (way == 0) {
 #pragma unroll
-    for (int w = 0; w < WAYS; ++w) { o += red[w][tid]; l += sums[w]; }
+    for (int w = 1; w < WAYS; ++w) f.add(1.f, sums[w], red[w][col]);
     const int64_t h = (int64_t)b * a.Hq + hg / a.NS * a.G + sub * kGMaxGroup + g;
-    put(reinterpret_cast<T*>(a.O) + h * D + WarpState<T, D, DAM_CODE_INT8>::dim_at(tid), l == 0.f ? 0.f : o / l);
-    if (tid == 0) a.lse[h] = lse_of(mx, l);
+    f.template write<D>(reinterpret_cast<T*>(a.O) + h * D, a.lse + h, 4 * col);
   }
 }
 
@@ -605,10 +649,11 @@ cache_join_kernel(CacheDecode a, DamCacheView c, const float* __restrict__ parti
 // As decode_group_kernel (dam_decode_mma.cu): one block, or a cluster of two to eight, per (sequence, KV head, group of 8 heads)
 // expands the patterns of its heads into one key list and deals its slices of 16 keys to the warps.
 constexpr int kMWarps = 5, kMStages = 2, kMBlocks = 4;
+constexpr int kScales = 2 * kSlice * 4;         // bytes of the scales of a slice
 
 template <int D>
 struct MaskedLayout {
-  static constexpr int ring = kMWarps * kMStages * Slice<D>::bytes;
+  static constexpr int ring = kMWarps * kMStages * (Slice<D>::bytes + kScales);
   static constexpr int merge = (kMWarps + 1) * kGMaxGroup * (D + 4) * 4;        // the merge reuses the ring
   static constexpr int codes_off = ring > merge ? ring : merge;                 // u16 per listed key: round-local word * 32 + bit
   static constexpr int words_off = codes_off + kGRoundWords * 32 * 2;           // u32 [head][round-local word]
@@ -660,7 +705,7 @@ cache_decode_masked_kernel(CacheDecode a, DamCacheView c, const unsigned char* _
   WS ws;
   ws.reset();
   ws.load_q(reinterpret_cast<const T*>(a.q) + ((int64_t)b * a.Hq + h0) * D, nh, a.scale_log2);
-  const uint32_t ring = static_cast<uint32_t>(__cvta_generic_to_shared(sm)) + warp * (kMStages * Slice<D>::bytes);
+  const uint32_t ring = static_cast<uint32_t>(__cvta_generic_to_shared(sm)) + warp * (kMStages * (Slice<D>::bytes + kScales));
   const uint64_t stream_policy = l2_evict_first_policy(), keep_policy = l2_evict_last_policy();
   for (int w0 = 0; w0 < nwords; w0 += kGRoundWords) {
     const int total = expand_round<kMWarps>(blob, H, sq, h0, nh, in_window, pos, w0, nwords, codes, whs, warp_tot, keep_policy);
@@ -670,7 +715,7 @@ cache_decode_masked_kernel(CacheDecode a, DamCacheView c, const unsigned char* _
     };
     const int nslices = (total + kSlice - 1) / kSlice, first = split * kMWarps + warp, step = nsplit * kMWarps;
     auto issue = [&](int s, int stage) {
-      const uint32_t dst = ring + stage * Slice<D>::bytes;
+      const uint32_t dst = ring + stage * (Slice<D>::bytes + kScales);
 #pragma unroll
       for (int i = 0; i < kSlice * Slice<D>::pieces / 32; ++i) {
         const int x = lane + 32 * i, r = x / Slice<D>::pieces, piece = x % Slice<D>::pieces, idx = s * kSlice + r;
@@ -680,7 +725,7 @@ cache_decode_masked_kernel(CacheDecode a, DamCacheView c, const unsigned char* _
         cp_async16(dst + Slice<D>::v_off + at, Vb + (int64_t)j * c.vst + piece * 16, stream_policy);
       }
       const int idx = s * kSlice + (lane & 15), j = key_of(codes[idx < total ? idx : s * kSlice]);
-      cp_async4_zfill(dst + Slice<D>::scale_off + 4 * lane, (lane < 16 ? c.ks : c.vs) + (row0 + (j >> c.shift)) * c.Hkv + kvh, 4u);
+      cp_async4_zfill(dst + Slice<D>::bytes + 4 * lane, (lane < 16 ? c.ks : c.vs) + (row0 + (j >> c.shift)) * c.Hkv + kvh, 4u);
     };
 #pragma unroll
     for (int s = 0; s < kMStages - 1; ++s) {
@@ -696,14 +741,15 @@ cache_decode_masked_kernel(CacheDecode a, DamCacheView c, const unsigned char* _
       uint32_t keep = 0u;
 #pragma unroll
       for (int k = 0; k < 2; ++k) {
-        const int idx = s * kSlice + row + 8 * k;
+        const int idx = s * kSlice + Slice<D>::key(row) + 8 * k;
         if (idx < total) {
           const uint32_t code = codes[idx];
 #pragma unroll
           for (int e = 0; e < 2; ++e) keep |= (whs[(2 * quad + e) * kGRoundWords + (code >> 5)] >> (code & 31u) & 1u) << (2 * k + e);
         }
       }
-      ws.template step<false, false>(ring + it % kMStages * Slice<D>::bytes, keep);
+      const uint32_t slice = ring + it % kMStages * (Slice<D>::bytes + kScales);
+      ws.template step<WS::kKeep>(slice, slice + Slice<D>::bytes, keep);
       __syncwarp();                                          // the stage is free for the copy the next trip issues
     }
     cp_async_wait<0>();                                      // (only empty groups are left; the merge reuses the ring)
@@ -714,51 +760,40 @@ cache_decode_masked_kernel(CacheDecode a, DamCacheView c, const unsigned char* _
   ws.store(mg + warp * (kGMaxGroup * WS::kRow));
   __syncthreads();
   float* folded = mg + kMWarps * kGMaxGroup * WS::kRow;
-  for (int e = tid; e < nh * D; e += kThreads) {
+  for (int e = 4 * tid; e < nh * D; e += 4 * kThreads) {
     const int g = e / D, p = e % D;
-    const float* src = mg + g * WS::kRow;
-    float mx = -CUDART_INF_F, lt = 0.f, ot = 0.f;
-#pragma unroll
-    for (int w = 0; w < kMWarps; ++w) mx = fmaxf(mx, src[w * (kGMaxGroup * WS::kRow) + D]);
-#pragma unroll
-    for (int w = 0; w < kMWarps; ++w) {
-      const float* sw = src + w * (kGMaxGroup * WS::kRow);
-      const float f = weight(sw[D], mx);
-      lt += sw[D + 1] * f;
-      ot += sw[p] * f;
-    }
+    Fold f;
+    f.template warps<kMWarps>(mg + g * WS::kRow, kGMaxGroup * WS::kRow, D, p);
     if constexpr (CLUSTER) {
-      folded[g * WS::kRow + p] = ot;
-      if (p == 0) { folded[g * WS::kRow + D] = mx; folded[g * WS::kRow + D + 1] = lt; }
+      *reinterpret_cast<float4*>(folded + g * WS::kRow + p) = f.o;
+      if (p == 0) { folded[g * WS::kRow + D] = f.m; folded[g * WS::kRow + D + 1] = f.l; }
     } else {
-      put(O + g * D + WS::dim_at(p), lt == 0.f ? 0.f : ot / lt);
-      if (p == 0) lse[g] = lse_of(mx, lt);
+      f.template write<D>(O + g * D, lse + g, p);
     }
   }
   if constexpr (CLUSTER) {
     cooperative_groups::cluster_group cl = cooperative_groups::this_cluster();
     cl.sync();
-    for (int e = split * kThreads + tid; e < nh * D; e += nsplit * kThreads) {
+    for (int e = 4 * (split * kThreads + tid); e < nh * D; e += 4 * nsplit * kThreads) {
       const int g = e / D, p = e % D;
-      float mv[kGMaxSplit], lv[kGMaxSplit], ov[kGMaxSplit], mx = -CUDART_INF_F;
+      float mv[kGMaxSplit], lv[kGMaxSplit];
+      float4 ov[kGMaxSplit];
+      Fold f;
+      f.m = -CUDART_INF_F; f.l = 0.f;
+      f.o = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
       for (int k = 0; k < kGMaxSplit; ++k) {
-        mv[k] = -CUDART_INF_F; lv[k] = ov[k] = 0.f;
+        mv[k] = -CUDART_INF_F; lv[k] = 0.f;
+        ov[k] = f.o;
         if (k < nsplit) {
           const float* src = cl.map_shared_rank(folded, k) + g * WS::kRow;
-          mv[k] = src[D]; lv[k] = src[D + 1]; ov[k] = src[p];
+          mv[k] = src[D]; lv[k] = src[D + 1]; ov[k] = *reinterpret_cast<const float4*>(src + p);
         }
-        mx = fmaxf(mx, mv[k]);
+        f.m = fmaxf(f.m, mv[k]);
       }
-      float lt = 0.f, ot = 0.f;
 #pragma unroll
-      for (int k = 0; k < kGMaxSplit; ++k) {
-        const float f = weight(mv[k], mx);
-        lt += lv[k] * f;
-        ot += ov[k] * f;
-      }
-      put(O + g * D + WS::dim_at(p), lt == 0.f ? 0.f : ot / lt);
-      if (p == 0) lse[g] = lse_of(mx, lt);
+      for (int k = 0; k < kGMaxSplit; ++k) f.add(weight(mv[k], f.m), lv[k], ov[k]);
+      f.template write<D>(O + g * D, lse + g, p);
     }
     cl.sync();                                               // the folded rows stay until every block has read them
   }
@@ -788,29 +823,38 @@ cudaError_t opt_in(int key, int* sm_count) {
 template <typename T, int D, int CODE> constexpr int kInstance = (sizeof(T) == 4) * 4 + (D == 128) * 2 + CODE;
 
 template <typename T, int D, int CODE>
-cudaError_t launch_dense(const CacheDecode& a, const DamCacheView& c, const dam_cache_t* cache, cudaStream_t st) {
-  constexpr int WARPS = 8, STAGES = D == 128 ? 5 : 8;
+cudaError_t launch_dense(CacheDecode a, const DamCacheView& c, const dam_cache_t* cache, cudaStream_t st) {
+  constexpr int WARPS = D == 128 ? 12 : 16, STAGES = D == 128 ? 3 : 4;
   using LY = DenseLayout<D, WARPS, STAGES>;
   int sms = 0;
   cudaError_t e = opt_in<cache_decode_kernel<T, D, CODE, WARPS, STAGES>, LY::total>(DAM_SETUP_CACHE_SMEM + kInstance<T, D, CODE>, &sms);
   if (e != cudaSuccess) return e;
-  // no more shares than there can be chunks
   const int64_t heads = (int64_t)c.Hkv * a.NS;
   int64_t most = 0, longest = 0;
   for (int b = 0; b < c.num_seqs; ++b) {
     const int64_t n = ((int64_t)cache->cu_seqlens_host[b + 1] - cache->cu_seqlens_host[b] + LY::chunk - 1) / LY::chunk;
-    most += n * heads;
+    most += n;
     longest = n > longest ? n : longest;
   }
-  if (most > 0x7FFFFFFF) return cudaErrorNotSupported;
-  int shares = sms < kMaxShares ? sms : kMaxShares;
-  if (most < shares) shares = most > 0 ? (int)most : 1;
+  if (most * heads > 0x7FFFFFFF) return cudaErrorNotSupported;
+  // all heads side by side where that leaves no more than an eighth of the SMs without work; and no more shares than there can be
+  // chunks
+  const int blocks = sms < kMaxShares ? sms : kMaxShares;
+  a.side = heads > 1 && heads <= blocks && blocks % heads * 8 <= blocks ? (int)heads : 1;
+  int64_t shares = blocks / a.side;
+  const int64_t list = a.side > 1 ? most : most * heads;
+  if (list < shares) shares = list > 0 ? list : 1;
+  CUtensorMap kmap, vmap;
+  if (!dam_make_tmap_codes(&kmap, c.k, D, c.Hkv, cache->total_tokens, c.kst, c.ksh, kSlice) ||
+      !dam_make_tmap_codes(&vmap, c.v, D, c.Hkv, cache->total_tokens, c.vst, c.vsh, kSlice))
+    return cudaErrorInvalidValue;
   float* partial = reinterpret_cast<float*>(a.scratch + 64);
-  e = dam_launch_chained(cache_decode_kernel<T, D, CODE, WARPS, STAGES>, dim3((unsigned)shares), dim3(WARPS * 32), LY::total, st, a, c, partial);
+  e = dam_launch_chained(cache_decode_kernel<T, D, CODE, WARPS, STAGES>, dim3((unsigned)(shares * a.side)), dim3(WARPS * 32), LY::total, st, kmap,
+                         vmap, a, c, partial);
   if (e != cudaSuccess || shares == 1 || longest <= 1) return e;   // (then every sequence is whole in one block)
   const int64_t grid = heads * (a.G < kGMaxGroup ? a.G : kGMaxGroup) * c.num_seqs;
   if (grid > 0x7FFFFFFF) return cudaErrorNotSupported;
-  return dam_launch_chained(cache_join_kernel<T, D>, dim3((unsigned)grid), dim3(256), 0, st, a, c, (const float*)partial, LY::chunk, shares);
+  return dam_launch_chained(cache_join_kernel<T, D>, dim3((unsigned)grid), dim3(256), 0, st, a, c, (const float*)partial, LY::chunk, (int)shares);
 }
 
 template <typename T, int D, int CODE>
@@ -851,6 +895,6 @@ cudaError_t dam_launch_cache_decode(const void* q, const dam_cache_t* cache, con
                                     float scale, void* O, float* lse, void* scratch, cudaStream_t st) {
   const int G = Hq / cache->num_kv_heads;
   const CacheDecode a = {q, positions, Hq, G, (G + kGMaxGroup - 1) / kGMaxGroup, scale * 1.4426950408889634f, O, lse,
-                         reinterpret_cast<uint32_t*>(scratch)};
+                         reinterpret_cast<uint32_t*>(scratch), 1};
   return DAM_CACHE_DISPATCH(launch, dtype, cache->head_dim, cache->code, a, cache, mask, st);
 }

@@ -248,3 +248,19 @@ inline bool dam_make_tmap_bf16(CUtensorMap* m, const void* base, int d, int head
                    CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   return r == CUDA_SUCCESS;
 }
+
+// 8-bit tensor [tokens][heads][d] (d = 64 or 128, contiguous) seen as 3-D (d, heads, tokens); box = d x 1 x rows, swizzled by the
+// row's bytes (128 or 64): one copy brings `rows` token rows of one head.  Strides in bytes.
+inline bool dam_make_tmap_codes(CUtensorMap* m, const void* base, int d, int heads, int64_t tokens, int64_t stride_tok, int64_t stride_head,
+                                int rows) {
+  dam_encode_tiled_fn enc = dam_get_encode_tiled();
+  if (!enc) return false;
+  cuuint64_t dims[3] = {(cuuint64_t)d, (cuuint64_t)heads, (cuuint64_t)(tokens > 0 ? tokens : 1)};
+  cuuint64_t strides[2] = {(cuuint64_t)stride_head, (cuuint64_t)stride_tok};
+  cuuint32_t box[3] = {(cuuint32_t)d, 1, (cuuint32_t)rows};
+  cuuint32_t estr[3] = {1, 1, 1};
+  CUresult r = enc(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 3, const_cast<void*>(base), dims, strides, box, estr,
+                   CU_TENSOR_MAP_INTERLEAVE_NONE, d == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B,
+                   CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  return r == CUDA_SUCCESS;
+}
