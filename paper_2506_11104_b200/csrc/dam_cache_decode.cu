@@ -26,6 +26,7 @@
 namespace {
 
 constexpr int kSlice = 16;             // keys of a slice: the rows of the first instruction, the k side of the second
+constexpr int kTile = 2;               // slices that a warp takes at a time where the keys are contiguous: two independent chains
 
 __device__ __forceinline__ void cp_async16_zfill(uint32_t dst, const void* src, uint32_t bytes) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
@@ -70,13 +71,13 @@ __device__ __forceinline__ void codes_to_half(uint32_t w, uint32_t* h) {
   }
 }
 
-// Rows of one slice in shared memory: 16 of K, 16 of V, as a tiled copy with 128-byte (head_dim 64: 64-byte) swizzle leaves them.
-// The 16-byte piece p of row r stands at piece p ^ (r & 7) of the row, for head_dim 64 at p ^ (r / 2 & 3): the eight lanes that a
-// 16-byte read is served for at a time find their pieces in different banks, given the order in which rows are taken.
-template <int D>
-struct Slice {
-  static constexpr int pieces = D / 16;
-  static constexpr int v_off = kSlice * D, bytes = 2 * kSlice * D;
+// Rows of N slices in shared memory: 16 N of K, 16 N of V, as a tiled copy with 128-byte (head_dim 64: 64-byte) swizzle leaves
+// them.  The 16-byte piece p of row r stands at piece p ^ (r & 7) of the row, for head_dim 64 at p ^ (r / 2 & 3): the eight lanes
+// that a 16-byte read is served for at a time find their pieces in different banks, given the order in which rows are taken.
+template <int D, int N>
+struct Rows {
+  static constexpr int keys = kSlice * N, pieces = D / 16;
+  static constexpr int v_off = keys * D, bytes = 2 * keys * D;
   static __device__ __forceinline__ uint32_t at(int r, int p) {
     if constexpr (D == 128) return r * 128 + ((p ^ (r & 7)) << 4);
     else return r * 64 + ((p ^ (r >> 1 & 3)) << 4);
@@ -107,25 +108,30 @@ struct WarpState {
     for (int u = 0; u < KS; ++u) o[u][0] = o[u][1] = o[u][2] = o[u][3] = 0.f;
   }
 
-  // q: row of the first head; `heads` of them exist
-  __device__ __forceinline__ void load_q(const T* q, int heads, float scale_log2) {
+  // The lane's elements of head `row`: dimensions D / 4 * quad ..., as they are in memory.  q: row of the first of `heads` heads.
+  struct Query { uint4 w[D / 4 * sizeof(T) / 16]; };
+  static __device__ __forceinline__ Query fetch_q(const T* q, int heads) {
     const int lane = threadIdx.x & 31, row = lane >> 2, quad = lane & 3;
-    constexpr int N = D / 4;                                 // the lane's elements of head `row`: dimensions N quad ...
+    const uint4* p = reinterpret_cast<const uint4*>(q + (int64_t)(row < heads ? row : 0) * D + D / 4 * quad);
+    Query r;
+#pragma unroll
+    for (int i = 0; i < (int)(sizeof(r.w) / 16); ++i) r.w[i] = __ldg(p + i);
+    return r;
+  }
+  __device__ __forceinline__ void set_q(const Query& q, int heads, float scale_log2) {
+    const int lane = threadIdx.x & 31, row = lane >> 2, quad = lane & 3;
+    constexpr int N = D / 4;
     float x[N];
-    const T* p = q + (int64_t)(row < heads ? row : 0) * D + N * quad;
-    if constexpr (kSplit) {
 #pragma unroll
-      for (int i = 0; i < N / 4; ++i) {
-        const float4 a = __ldg(reinterpret_cast<const float4*>(p) + i);
-        x[4 * i] = a.x; x[4 * i + 1] = a.y; x[4 * i + 2] = a.z; x[4 * i + 3] = a.w;
-      }
-    } else {
+    for (int i = 0; i < (int)(sizeof(q.w) / 16); ++i) {
+      const uint32_t w[4] = {q.w[i].x, q.w[i].y, q.w[i].z, q.w[i].w};
 #pragma unroll
-      for (int i = 0; i < N / 8; ++i) {
-        const uint4 a = __ldg(reinterpret_cast<const uint4*>(p) + i);
-        const uint32_t w[4] = {a.x, a.y, a.z, a.w};
-#pragma unroll
-        for (int k = 0; k < 4; ++k) { x[8 * i + 2 * k] = __uint_as_float(w[k] << 16); x[8 * i + 2 * k + 1] = __uint_as_float(w[k] & 0xFFFF0000u); }
+      for (int k = 0; k < 4; ++k) {
+        if constexpr (kSplit) {
+          x[4 * i + k] = __uint_as_float(w[k]);
+        } else {
+          x[8 * i + 2 * k] = __uint_as_float(w[k] << 16); x[8 * i + 2 * k + 1] = __uint_as_float(w[k] & 0xFFFF0000u);
+        }
       }
     }
     uint32_t top = 0u;
@@ -153,54 +159,82 @@ struct WarpState {
     qs[1] = __shfl_sync(0xFFFFFFFFu, back, 8 * quad + 4);
   }
 
-  // One slice: rows at `slice`, scales at `sc`, and which keys there are for whom.
-  //   kAll    every head keeps all 16; they share their scales, K's and V's (they lie in one block)
-  //   kFirst  the same for the first `arg` of them; the rows behind may hold anything
-  //   kKeep   bit e (e + 2) of arg: head 2 quad + e keeps key `row` (key `row + 8`), keys by Slice::key; 16 scales of K and of V
+  // N slices: rows at `rows`, scales at `sc`, and which keys there are for whom.
+  //   kAll    every head keeps all of them; the 16 of a slice share their scales (they lie in one block): K's and V's, slice by slice
+  //   kFirst  the same for the first `arg` keys; the rows behind may hold anything
+  //   kKeep   (one slice) bit e (e + 2) of arg: head 2 quad + e keeps key `row` (key `row + 8`), keys by Rows::key; 16 scales of K and
+  //           16 of V
   // A key that a head does not keep has no part in it.
   enum Mode { kAll, kFirst, kKeep };
-  template <Mode MODE>
-  __device__ __forceinline__ void step(uint32_t slice, uint32_t sc, uint32_t arg) {
-    using SL = Slice<D>;
+  template <Mode MODE, int N>
+  __device__ __forceinline__ void step(uint32_t rows, uint32_t sc, uint32_t arg) {
+    using RW = Rows<D, N>;
     constexpr bool ALL = MODE == kAll, UNIFORM = MODE != kKeep;
-    const int lane = threadIdx.x & 31, row = lane >> 2, quad = lane & 3, key = SL::key(row);
-    uint32_t keep = arg;
-    if constexpr (MODE == kFirst) keep = (key < (int)arg ? 3u : 0u) | (key + 8 < (int)arg ? 12u : 0u);
-    const float ks0 = lds_float(sc + (UNIFORM ? 0 : 4 * key)), vs0 = lds_float(sc + (UNIFORM ? 4 : 64 + 4 * key));
-    const float ks1 = UNIFORM ? ks0 : lds_float(sc + 32 + 4 * key), vs1 = UNIFORM ? vs0 : lds_float(sc + 96 + 4 * key);
-    auto kept = [&](int bit) { return ALL || (keep >> bit & 1u); };
-    // S^T = K q^T: k-step s takes the dimensions D / 4 * quad + 4 s ... of a lane
-    float st[2][4] = {};                                     // (two chains of instructions, half as long)
+    static_assert(UNIFORM || N == 1, "keys of their own come one slice at a time");
+    const int lane = threadIdx.x & 31, row = lane >> 2, quad = lane & 3, key = RW::key(row);
+    uint32_t keep[N];
+    float ks[N][2], vs[N][2];                                // of keys row and row + 8
 #pragma unroll
-    for (int c = 0; c < D / 64; ++c) {
-      const uint4 a = lds128(slice + SL::at(key, D / 64 * quad + c)), b = lds128(slice + SL::at(key + 8, D / 64 * quad + c));
-      const uint32_t wa[4] = {a.x, a.y, a.z, a.w}, wb[4] = {b.x, b.y, b.z, b.w};
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int s = 4 * c + i;
-        uint32_t ha[2], hb[2];
-        codes_to_half<CODE>(wa[i], ha);
-        codes_to_half<CODE>(wb[i], hb);
-        mma_f16(st[s & 1], ha[0], hb[0], ha[1], hb[1], qh[s][0], qh[s][1]);
-        if constexpr (kSplit) mma_f16(st[s & 1], ha[0], hb[0], ha[1], hb[1], ql[s][0], ql[s][1]);
+    for (int n = 0; n < N; ++n) {
+      keep[n] = arg;
+      if constexpr (MODE == kFirst) keep[n] = (16 * n + key < (int)arg ? 3u : 0u) | (16 * n + key + 8 < (int)arg ? 12u : 0u);
+      if constexpr (UNIFORM) {
+        ks[n][0] = ks[n][1] = lds_float(sc + 8 * n);
+        vs[n][0] = vs[n][1] = lds_float(sc + 8 * n + 4);
+      } else {
+        ks[n][0] = lds_float(sc + 4 * key); ks[n][1] = lds_float(sc + 32 + 4 * key);
+        vs[n][0] = lds_float(sc + 64 + 4 * key); vs[n][1] = lds_float(sc + 96 + 4 * key);
       }
     }
-    float x[4];
+    auto kept = [&](int n, int bit) { return ALL || (keep[n] >> bit & 1u); };
+    // S^T = K q^T: k-step s takes the dimensions D / 4 * quad + 4 s ... of a lane
+    float st[N][2][4] = {};                                  // (two chains of instructions per slice, half as long)
 #pragma unroll
-    for (int e = 0; e < 2; ++e) {
-      x[e] = kept(e) ? (st[0][e] + st[1][e]) * (ks0 * qs[e]) : -CUDART_INF_F;
-      x[2 + e] = kept(2 + e) ? (st[0][2 + e] + st[1][2 + e]) * (ks1 * qs[e]) : -CUDART_INF_F;
+    for (int c = 0; c < D / 64; ++c) {
+#pragma unroll
+      for (int n = 0; n < N; ++n) {
+        const uint4 a = lds128(rows + RW::at(16 * n + key, D / 64 * quad + c)), b = lds128(rows + RW::at(16 * n + key + 8, D / 64 * quad + c));
+        const uint32_t wa[4] = {a.x, a.y, a.z, a.w}, wb[4] = {b.x, b.y, b.z, b.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int s = 4 * c + i;
+          uint32_t ha[2], hb[2];
+          codes_to_half<CODE>(wa[i], ha);
+          codes_to_half<CODE>(wb[i], hb);
+          mma_f16(st[n][s & 1], ha[0], hb[0], ha[1], hb[1], qh[s][0], qh[s][1]);
+          if constexpr (kSplit) mma_f16(st[n][s & 1], ha[0], hb[0], ha[1], hb[1], ql[s][0], ql[s][1]);
+        }
+      }
+    }
+    float x[N][4], c[N][2];
+    bool far = false;
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        x[n][e] = kept(n, e) ? (st[n][0][e] + st[n][1][e]) * (ks[n][0] * qs[e]) : -CUDART_INF_F;
+        x[n][2 + e] = kept(n, 2 + e) ? (st[n][0][2 + e] + st[n][1][2 + e]) * (ks[n][1] * qs[e]) : -CUDART_INF_F;
+      }
+      c[n][0] = vs[n][0] * vinv;
+      c[n][1] = UNIFORM ? c[n][0] : vs[n][1] * vinv;
+      // (one that is not kept does not count; a slice of the first keys may have none)
+      far |= ((ALL || keep[n] & 3u) && c[n][0] > 128.f) || (!UNIFORM && (keep[n] & 12u) && c[n][1] > 128.f);
     }
     // The reference of the logits moves when one lies more than 8 above it (probabilities stay below 2^8), that of the V scales
-    // when one reaches 128 times it: most slices move nothing.
-    float c0 = vs0 * vinv, c1 = UNIFORM ? c0 : vs1 * vinv;
-    const bool far = fmaxf(x[0], x[2]) > m[0] + 8.f || fmaxf(x[1], x[3]) > m[1] + 8.f;
-    const bool large = ((ALL || keep & 3u) && c0 > 128.f) || (!UNIFORM && (ALL || keep & 12u) && c1 > 128.f);
-    if (__any_sync(0xFFFFFFFFu, far || large)) {
+    // when one reaches 128 times it: most steps move nothing.
+    float top[2];
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      top[e] = fmaxf(x[0][e], x[0][2 + e]);
+#pragma unroll
+      for (int n = 1; n < N; ++n) top[e] = fmaxf(top[e], fmaxf(x[n][e], x[n][2 + e]));
+      far |= top[e] > m[e] + 8.f;
+    }
+    if (__any_sync(0xFFFFFFFFu, far)) {
       float f[2];
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
-        float mx = fmaxf(x[e], x[2 + e]);
+        float mx = top[e];
         mx = fmaxf(mx, __shfl_xor_sync(0xFFFFFFFFu, mx, 4));
         mx = fmaxf(mx, __shfl_xor_sync(0xFFFFFFFFu, mx, 8));
         mx = fmaxf(mx, __shfl_xor_sync(0xFFFFFFFFu, mx, 16));
@@ -209,68 +243,79 @@ struct WarpState {
         m[e] = mn;
         l[e] *= f[e];
       }
-      float top = fmaxf(ALL || keep & 3u ? vs0 : 0.f, ALL || keep & 12u ? vs1 : 0.f);
+      float vt = 0.f;
 #pragma unroll
-      for (int d = 1; d < 32; d <<= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, d));
-      if (top * vinv > 128.f) {
-        const int n = max(1, min(234, 260 - (int)(__float_as_uint(top) >> 23)));   // top * 2^(n - 127) lies in [64, 128)
-        const float now = __uint_as_float((uint32_t)n << 23), ratio = now / vinv;
+      for (int n = 0; n < N; ++n) vt = fmaxf(vt, fmaxf(ALL || keep[n] & 3u ? vs[n][0] : 0.f, ALL || keep[n] & 12u ? vs[n][1] : 0.f));
+#pragma unroll
+      for (int d = 1; d < 32; d <<= 1) vt = fmaxf(vt, __shfl_xor_sync(0xFFFFFFFFu, vt, d));
+      if (vt * vinv > 128.f) {
+        const int b = max(1, min(234, 260 - (int)(__float_as_uint(vt) >> 23)));   // vt * 2^(b - 127) lies in [64, 128)
+        const float now = __uint_as_float((uint32_t)b << 23), ratio = now / vinv;
         vinv = now;
-        c0 = vs0 * vinv; c1 = vs1 * vinv;
         f[0] *= ratio; f[1] *= ratio;
+#pragma unroll
+        for (int n = 0; n < N; ++n) { c[n][0] = vs[n][0] * vinv; c[n][1] = vs[n][1] * vinv; }
       }
 #pragma unroll
       for (int u = 0; u < KS; ++u) { o[u][0] *= f[0]; o[u][1] *= f[1]; o[u][2] *= f[0]; o[u][3] *= f[1]; }
     }
-    float w[4];
+    uint32_t pb[N][2], pl[N][2];
+    // (no key yet, or logits of -inf alone: no weight)
+    const float ref[2] = {m[0] == -CUDART_INF_F ? 0.f : m[0], m[1] == -CUDART_INF_F ? 0.f : m[1]};
 #pragma unroll
-    for (int e = 0; e < 2; ++e) {
-      const float ref = m[e] == -CUDART_INF_F ? 0.f : m[e];  // (no key yet, or logits of -inf alone: no weight)
-      const float p0 = g_ex2(x[e] - ref), p1 = g_ex2(x[2 + e] - ref);
-      l[e] += p0 + p1;
-      // (a key that is not kept may stand in a block without a scale: 0 * NaN is not 0)
-      w[e] = kept(e) ? p0 * c0 : 0.f;
-      w[2 + e] = kept(2 + e) ? p1 * c1 : 0.f;
-    }
-    // P^T as operands (k = key, n = head): the transposes of the two 8 x 8 blocks [key][head]
-    const uint32_t h0 = pack_half2(w[0], w[1]), h1 = pack_half2(w[2], w[3]);
-    const uint32_t pb0 = movmatrix_trans(h0), pb1 = movmatrix_trans(h1);
-    uint32_t pl0 = 0u, pl1 = 0u;
-    if constexpr (kSplit) {
-      const float2 f0 = __half22float2(*reinterpret_cast<const __half2*>(&h0)), f1 = __half22float2(*reinterpret_cast<const __half2*>(&h1));
-      pl0 = movmatrix_trans(pack_half2(w[0] - f0.x, w[1] - f0.y));
-      pl1 = movmatrix_trans(pack_half2(w[2] - f1.x, w[3] - f1.y));
+    for (int n = 0; n < N; ++n) {
+      float w[4];
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const float p0 = g_ex2(x[n][e] - ref[e]), p1 = g_ex2(x[n][2 + e] - ref[e]);
+        l[e] += p0 + p1;
+        // (a key that is not kept may stand in a block without a scale: 0 * NaN is not 0)
+        w[e] = kept(n, e) ? p0 * c[n][0] : 0.f;
+        w[2 + e] = kept(n, 2 + e) ? p1 * c[n][1] : 0.f;
+      }
+      // P^T as operands (k = key, n = head): the transposes of the two 8 x 8 blocks [key][head]
+      const uint32_t h0 = pack_half2(w[0], w[1]), h1 = pack_half2(w[2], w[3]);
+      pb[n][0] = movmatrix_trans(h0);
+      pb[n][1] = movmatrix_trans(h1);
+      if constexpr (kSplit) {
+        const float2 f0 = __half22float2(*reinterpret_cast<const __half2*>(&h0)), f1 = __half22float2(*reinterpret_cast<const __half2*>(&h1));
+        pl[n][0] = movmatrix_trans(pack_half2(w[0] - f0.x, w[1] - f0.y));
+        pl[n][1] = movmatrix_trans(pack_half2(w[2] - f1.x, w[3] - f1.y));
+      }
     }
     // O^T += V^T P^T: the lane's rows are 2 quad, 2 quad + 1, 2 quad + 8, 2 quad + 9; their codes of one dimension are brought
     // together byte by byte
-    uint32_t vw[4][D / 32];
 #pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      const int at = SL::key(2 * quad + (r & 1)) + (r >> 1) * 8;
-      if constexpr (D == 128) {
-        const uint4 a = lds128(slice + SL::v_off + SL::at(at, row));
-        vw[r][0] = a.x; vw[r][1] = a.y; vw[r][2] = a.z; vw[r][3] = a.w;
-      } else {
-        const uint2 a = lds64(slice + SL::v_off + SL::at(at, row >> 1) + (row & 1) * 8);
-        vw[r][0] = a.x; vw[r][1] = a.y;
+    for (int n = 0; n < N; ++n) {
+      uint32_t vw[4][D / 32];
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int at = 16 * n + RW::key(2 * quad + (r & 1)) + (r >> 1) * 8;
+        if constexpr (D == 128) {
+          const uint4 a = lds128(rows + RW::v_off + RW::at(at, row));
+          vw[r][0] = a.x; vw[r][1] = a.y; vw[r][2] = a.z; vw[r][3] = a.w;
+        } else {
+          const uint2 a = lds64(rows + RW::v_off + RW::at(at, row >> 1) + (row & 1) * 8);
+          vw[r][0] = a.x; vw[r][1] = a.y;
+        }
+        if constexpr (MODE == kFirst) {                      // (an e4m3 code behind the last key may be a NaN: 0 * NaN is not 0)
+#pragma unroll
+          for (int i = 0; i < D / 32; ++i) vw[r][i] = at < (int)arg ? vw[r][i] : 0u;
+        }
       }
-      if constexpr (MODE == kFirst) {                        // (an e4m3 code behind the last key may be a NaN: 0 * NaN is not 0)
 #pragma unroll
-        for (int i = 0; i < D / 32; ++i) vw[r][i] = at < (int)arg ? vw[r][i] : 0u;
-      }
-    }
+      for (int i = 0; i < D / 32; ++i) {
 #pragma unroll
-    for (int i = 0; i < D / 32; ++i) {
-#pragma unroll
-      for (int k = 0; k < 2; ++k) {
-        // (bytes 2 k, 2 k + 1 of either key: dimension 4 i + 2 k of both keys, then dimension 4 i + 2 k + 1)
-        const uint32_t sel = k ? 0x7362u : 0x5140u;
-        uint32_t a[2], b[2];
-        codes_to_half<CODE>(__byte_perm(vw[0][i], vw[1][i], sel), a);
-        codes_to_half<CODE>(__byte_perm(vw[2][i], vw[3][i], sel), b);
-        const int u = 2 * i + k;
-        mma_f16(o[u], a[0], a[1], b[0], b[1], pb0, pb1);
-        if constexpr (kSplit) mma_f16(o[u], a[0], a[1], b[0], b[1], pl0, pl1);
+        for (int k = 0; k < 2; ++k) {
+          // (bytes 2 k, 2 k + 1 of either key: dimension 4 i + 2 k of both keys, then dimension 4 i + 2 k + 1)
+          const uint32_t sel = k ? 0x7362u : 0x5140u;
+          uint32_t a[2], b[2];
+          codes_to_half<CODE>(__byte_perm(vw[0][i], vw[1][i], sel), a);
+          codes_to_half<CODE>(__byte_perm(vw[2][i], vw[3][i], sel), b);
+          const int u = 2 * i + k;
+          mma_f16(o[u], a[0], a[1], b[0], b[1], pb[n][0], pb[n][1]);
+          if constexpr (kSplit) mma_f16(o[u], a[0], a[1], b[0], b[1], pl[n][0], pl[n][1]);
+        }
       }
     }
   }
@@ -335,6 +380,36 @@ struct Fold {
   }
 };
 
+// The folded rows ([head][stride]: O, reference, sum) of the blocks of a cluster, at most MOST of them, to the result.
+template <int D, int MOST, typename T>
+__device__ __forceinline__ void fold_cluster(float* folded, int stride, int heads, int threads, T* O, float* lse) {
+  cooperative_groups::cluster_group cl = cooperative_groups::this_cluster();
+  const int blocks = (int)cl.num_blocks(), rank = (int)cl.block_rank();
+  cl.sync();
+  for (int e = 4 * (rank * threads + (int)threadIdx.x); e < heads * D; e += 4 * blocks * threads) {
+    const int g = e / D, p = e % D;
+    float mv[MOST], lv[MOST];
+    float4 ov[MOST];
+    Fold f;
+    f.m = -CUDART_INF_F; f.l = 0.f;
+    f.o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+    for (int k = 0; k < MOST; ++k) {
+      mv[k] = -CUDART_INF_F; lv[k] = 0.f;
+      ov[k] = f.o;
+      if (k < blocks) {
+        const float* src = cl.map_shared_rank(folded, k) + g * stride;
+        mv[k] = src[D]; lv[k] = src[D + 1]; ov[k] = *reinterpret_cast<const float4*>(src + p);
+      }
+      f.m = fmaxf(f.m, mv[k]);
+    }
+#pragma unroll
+    for (int k = 0; k < MOST; ++k) f.add(weight(mv[k], f.m), lv[k], ov[k]);
+    f.template write<D>(O + g * D, lse + g, p);
+  }
+  cl.sync();                                                 // the folded rows stay until every block has read them
+}
+
 struct CacheDecode {
   const void* q;
   const int32_t* pos;
@@ -347,7 +422,7 @@ struct CacheDecode {
 };
 
 // ---- every key ----------------------------------------------------------------------------------
-// The keys of all sequences form one list of chunks (WARPS slices: one per warp), and share s of S takes the chunks [total s / S,
+// The keys of all sequences form one list of chunks (a tile of 32 keys per warp), and share s of S takes the chunks [total s / S,
 // total (s + 1) / S): every SM reads the same number of bytes, however ragged the batch.  side > 1: that many (KV head, group of 8
 // heads), all of them, are served side by side, a block for each in every share: the rows that neighbouring blocks read at about the
 // same time are neighbours in memory.  side == 1: the list goes through the (KV head, group) of each sequence one after the other.
@@ -359,20 +434,27 @@ __device__ __forceinline__ int chunks_of(const DamCacheView& c, const int32_t* p
   return (unsigned)p >= (unsigned)room ? 0 : p / chunk + 1;
 }
 
+constexpr int kKeys = kTile * kSlice;    // keys of a warp's tile
+
 // Chunks per head of all sequences, of those before sequence b, and whether some position lies outside its capacity (whole warp).
 struct Survey {
-  int total, before;
+  int total, before, mine;     // mine: chunks of sequence `lane`
   bool bad;
-  __device__ __forceinline__ Survey(const DamCacheView& c, const int32_t* pos, int chunk, int b) : total(0), before(0), bad(false) {
-    for (int base = 0; base < c.num_seqs; base += 32) {
-      const int x = base + (threadIdx.x & 31);
-      const int n = x < c.num_seqs ? chunks_of(c, pos, x, chunk) : -1;
-      bad |= __any_sync(0xFFFFFFFFu, n == 0);
-      total += max(n, 0);
-      before += x < b ? max(n, 0) : 0;
+  __device__ __forceinline__ Survey(const DamCacheView& c, const int32_t* pos, int chunk, int b) : bad(false) {
+    const int lane = threadIdx.x & 31;
+    mine = lane < c.num_seqs ? chunks_of(c, pos, lane, chunk) : 0;
+    bad = lane < c.num_seqs && mine == 0;
+    total = mine;
+    before = lane < b ? mine : 0;
+    for (int x = 32 + lane; x < c.num_seqs; x += 32) {
+      const int n = chunks_of(c, pos, x, chunk);
+      bad |= n == 0;
+      total += n;
+      before += x < b ? n : 0;
     }
     total = __reduce_add_sync(0xFFFFFFFFu, total);
     before = __reduce_add_sync(0xFFFFFFFFu, before);
+    bad = __any_sync(0xFFFFFFFFu, bad);
   }
 };
 
@@ -380,21 +462,18 @@ struct Survey {
 struct Place {
   int b, hg;                   // sequence; KV head and group of heads
   int n, left;                 // chunks of the sequence, and how many are left of this (KV head, group), this one included
-  int live;                    // keys of the sequence from the warp's slice of this chunk on (may be none: <= 0)
-  __device__ __forceinline__ void enter(const DamCacheView& c, const int32_t* pos, int b_, int chunk) {
-    b = b_;
-    n = chunks_of(c, pos, b, chunk);
-  }
+  int live;                    // keys of the sequence from the warp's tile of this chunk on (may be none: <= 0)
   __device__ __forceinline__ void begin(const int32_t* pos, int chunk, int k) {
     left = n - k;
-    live = __ldg(pos + b) + 1 - k * chunk - (int)(threadIdx.x >> 5) * kSlice;
+    live = __ldg(pos + b) + 1 - k * chunk - (int)(threadIdx.x >> 5) * kKeys;
   }
   // chunk `at` of the whole list (which has it); returns its number within the (KV head, group)
-  __device__ __forceinline__ int locate(const DamCacheView& c, const int32_t* pos, int chunk, int heads, int at) {
+  __device__ __forceinline__ int locate(const DamCacheView& c, const int32_t* pos, const Survey& all, int chunk, int heads, int at) {
     const int lane = threadIdx.x & 31;
-    int before = 0;
+    int before = 0, mine = all.mine;
+    b = hg = 0; n = left = 1; live = 0;
     for (int base = 0; base < c.num_seqs; base += 32) {
-      const int mine = base + lane < c.num_seqs ? chunks_of(c, pos, base + lane, chunk) : 0;   // (read before: in the L1 cache)
+      if (base) mine = base + lane < c.num_seqs ? chunks_of(c, pos, base + lane, chunk) : 0;
       int incl = mine;
 #pragma unroll
       for (int o = 1; o < 32; o <<= 1) {
@@ -404,16 +483,18 @@ struct Place {
       const uint32_t past = __ballot_sync(0xFFFFFFFFu, (before + incl) * heads > at);
       if (past) {
         const int w = __ffs(past) - 1;
-        const int first = (before + __shfl_sync(0xFFFFFFFFu, incl - mine, w)) * heads;
-        enter(c, pos, base + w, chunk);
-        hg = (at - first) / n;
-        const int k = (at - first) % n;
+        b = base + w;
+        n = __shfl_sync(0xFFFFFFFFu, mine, w);
+        int k = at - (before + __shfl_sync(0xFFFFFFFFu, incl, w) - n) * heads;
+        if (heads > 1) {
+          hg = k / n;
+          k -= hg * n;
+        }
         begin(pos, chunk, k);
         return k;
       }
       before += __shfl_sync(0xFFFFFFFFu, incl, 31);
     }
-    b = hg = 0; n = left = 1; live = 0;                       // (not reached)
     return 0;
   }
   // the next chunk (there is one); whether it is another (KV head, group)'s first
@@ -424,7 +505,7 @@ struct Place {
     }
     if (++hg == heads) {
       hg = 0;
-      do { enter(c, pos, b + 1, chunk); } while (n == 0 && b + 1 < c.num_seqs);
+      do { n = chunks_of(c, pos, ++b, chunk); } while (n == 0 && b + 1 < c.num_seqs);
     }
     begin(pos, chunk, 0);
     return true;
@@ -433,11 +514,11 @@ struct Place {
 
 template <int D, int WARPS, int STAGES>
 struct DenseLayout {
-  static constexpr int chunk = WARPS * kSlice;
-  static constexpr int ring = WARPS * STAGES * Slice<D>::bytes;
+  static constexpr int chunk = WARPS * kKeys;
+  static constexpr int ring = WARPS * STAGES * Rows<D, kTile>::bytes;
   static constexpr int merge_off = ring, merge = WARPS * kGMaxGroup * (D + 4) * 4;
-  static constexpr int scale_off = merge_off + merge;                           // [warp][stage] K scale, V scale
-  static constexpr int bar_off = scale_off + WARPS * STAGES * 8;                // [warp][stage]
+  static constexpr int scale_off = merge_off + merge;                           // [warp][stage][slice] K scale, V scale
+  static constexpr int bar_off = scale_off + WARPS * STAGES * kTile * 8;        // [warp][stage]
   static constexpr int flag_off = bar_off + WARPS * STAGES * 8;
   static constexpr int total = flag_off + 16 + 1024;                            // (the ring starts on a multiple of 1024)
 };
@@ -467,8 +548,8 @@ cache_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_const
   const int share = blockIdx.x / a.side, beside = blockIdx.x - share * a.side;
   unsigned char* sm = sm_raw + (-sm100::smem_u32(sm_raw) & 1023u);
   float* mg = reinterpret_cast<float*>(sm + LY::merge_off);
-  const uint32_t base = sm100::smem_u32(sm), ring = base + warp * (STAGES * Slice<D>::bytes);
-  const uint32_t scales = base + LY::scale_off + warp * (STAGES * 8), bars = base + LY::bar_off + warp * (STAGES * 8);
+  const uint32_t base = sm100::smem_u32(sm), ring = base + warp * (STAGES * Rows<D, kTile>::bytes);
+  const uint32_t scales = base + LY::scale_off + warp * (STAGES * kTile * 8), bars = base + LY::bar_off + warp * (STAGES * 8);
   volatile uint32_t* const gave_up = reinterpret_cast<uint32_t*>(sm + LY::flag_off);
   if (lane < STAGES) sm100::mbar_init(bars + 8 * lane, 1);
   if (tid == 0) {
@@ -495,33 +576,36 @@ cache_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_const
   const int lo = sh.begin(share), todo = sh.begin(share + 1) - lo;
   if (todo == 0) return;
   Place in, cur;
-  int key = in.locate(c, a.pos, LY::chunk, heads, lo) * LY::chunk + warp * kSlice;     // first key of the slice to be copied
+  int key = in.locate(c, a.pos, all, LY::chunk, heads, lo) * LY::chunk + warp * kKeys;     // first key of the slice to be copied
   cur = in;
 
-  // The copies: a tile of 16 rows of K, one of V, and their two scales (lanes 0 and 16).
+  // The copies: a tile of 32 rows of K, one of V, and the scales of its two slices.
   const float* sp;                     // scale of block 0 of the sequence
   int kvh, token;                      // KV head; packed row of the slice's first key
   auto aim = [&]() {
-    kvh = (in.hg + beside) / a.NS;
+    kvh = a.NS == 1 ? in.hg + beside : (in.hg + beside) / a.NS;
     const int cu = __ldg(c.cu + in.b);
     token = cu + key;
-    sp = (lane < 16 ? c.ks : c.vs) + (int64_t)((cu >> c.shift) + in.b) * c.Hkv + kvh;
+    sp = (lane & 1 ? c.vs : c.ks) + (int64_t)((cu >> c.shift) + in.b) * c.Hkv + kvh;
   };
   auto issue = [&](int stage) {
     if (in.live <= 0) return;
     // (16 keys from a multiple of 16 on lie in one block.  A tile may reach into the rows behind the last key, of this sequence
-    // or of the next; rows beyond the cache read as zeros)
-    if ((lane & 15) == 0) cp_async4_zfill(scales + 8 * stage + (lane >> 2), sp + (int64_t)(key >> c.shift) * c.Hkv, 4u);
+    // or of the next; rows beyond the cache read as zeros.  The scale of a slice without a key is the first slice's)
+    if (lane < 2 * kTile) {
+      const int at = key + (in.live > (lane >> 1) * kSlice ? (lane >> 1) * kSlice : 0);
+      cp_async4_zfill(scales + 8 * kTile * stage + 4 * lane, sp + (int64_t)(at >> c.shift) * c.Hkv, 4u);
+    }
     if (sm100::elect_one()) {
-      const uint32_t dst = ring + stage * Slice<D>::bytes, bar = bars + 8 * stage;
-      sm100::mbar_arrive_expect_tx(bar, Slice<D>::bytes);
+      const uint32_t dst = ring + stage * Rows<D, kTile>::bytes, bar = bars + 8 * stage;
+      sm100::mbar_arrive_expect_tx(bar, Rows<D, kTile>::bytes);
       sm100::tma_load_3d(dst, &kmap, bar, 0, kvh, token);
-      sm100::tma_load_3d(dst + Slice<D>::v_off, &vmap, bar, 0, kvh, token);
+      sm100::tma_load_3d(dst + Rows<D, kTile>::v_off, &vmap, bar, 0, kvh, token);
     }
   };
   auto advance = [&]() {
     if (in.next(c, a.pos, LY::chunk, heads)) {
-      key = warp * kSlice;
+      key = warp * kKeys;
       aim();
     } else {
       token += LY::chunk;
@@ -551,20 +635,20 @@ cache_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_const
     }
     cp_async_commit();
     if (since == 0) {
-      const int kv = (cur.hg + beside) / a.NS, sub = cur.hg + beside - kv * a.NS;
+      const int kv = a.NS == 1 ? cur.hg + beside : (cur.hg + beside) / a.NS, sub = cur.hg + beside - kv * a.NS;
       h0 = kv * a.G + sub * kGMaxGroup;
       nh = min(kGMaxGroup, a.G - sub * kGMaxGroup);
       ws.reset();
-      ws.load_q(reinterpret_cast<const T*>(a.q) + ((int64_t)cur.b * a.Hq + h0) * D, nh, a.scale_log2);
+      ws.set_q(WS::fetch_q(reinterpret_cast<const T*>(a.q) + ((int64_t)cur.b * a.Hq + h0) * D, nh), nh, a.scale_log2);
     }
     cp_async_wait<STAGES - 1>();
     __syncwarp();
     if (cur.live > 0 && !lost) {
       lost = !sm100::mbar_wait(bars + 8 * stage, phases >> stage & 1u, gave_up);
       phases ^= 1u << stage;
-      const uint32_t slice = ring + stage * Slice<D>::bytes, sc = scales + 8 * stage;
-      if (cur.live >= kSlice) ws.template step<WS::kAll>(slice, sc, 15u);
-      else ws.template step<WS::kFirst>(slice, sc, (uint32_t)cur.live);
+      const uint32_t rows = ring + stage * Rows<D, kTile>::bytes, sc = scales + 8 * kTile * stage;
+      if (cur.live >= kKeys) ws.template step<WS::kAll, kTile>(rows, sc, 0u);
+      else ws.template step<WS::kFirst, kTile>(rows, sc, (uint32_t)cur.live);
     }
     __syncwarp();                                            // the stage is free for the copy the next trip issues
     stage = stage + 1 == STAGES ? 0 : stage + 1;
@@ -604,13 +688,13 @@ __global__ void __launch_bounds__(256)
 cache_join_kernel(CacheDecode a, DamCacheView c, const float* __restrict__ partial, int chunk, int shares) {
   constexpr int TD = D / 4, WAYS = 256 / TD;                 // threads of a row (4 positions each), partial results at a time
   __shared__ float4 red[WAYS][TD];
-  __shared__ float sums[WAYS];
+  __shared__ float sums[WAYS], refs[WAYS];
   // (before the wait: the positions, which the kernel before this one has read behind its own wait; it writes none)
   asm volatile("griddepcontrol.launch_dependents;");
   const int heads = c.Hkv * a.NS, per = min(a.G, kGMaxGroup);
   const int g = blockIdx.x % per, hg = blockIdx.x / per % heads, b = blockIdx.x / per / heads;
   const int sub = hg % a.NS, nh = min(kGMaxGroup, a.G - sub * kGMaxGroup);
-  const int tid = threadIdx.x, lane = tid & 31, way = tid / TD, col = tid % TD;
+  const int tid = threadIdx.x, way = tid / TD, col = tid % TD;
   const int n = chunks_of(c, a.pos, b, chunk);
   const Survey all(c, a.pos, chunk, b);
   const int list = a.side > 1 ? 1 : heads;
@@ -623,26 +707,163 @@ cache_join_kernel(CacheDecode a, DamCacheView c, const float* __restrict__ parti
     const int block = a.side > 1 ? s * a.side + hg : s;
     return partial + (int64_t)(2 * block + (sh.begin(s) < first)) * kPartial<D>;
   };
+  // every thread joins its share of them under a reference of its own
   Fold f;
   f.m = -CUDART_INF_F; f.l = 0.f;
   f.o = make_float4(0.f, 0.f, 0.f, 0.f);
-  for (int s = s0 + lane; s <= s1; s += 32) f.m = fmaxf(f.m, row_of(s)[kGMaxGroup * D + g]);
+  for (int s = s0 + way; s <= s1; s += 4 * WAYS) {
+    float m[4], l[4], mx = f.m;
+    float4 o[4];
 #pragma unroll
-  for (int o = 1; o < 32; o <<= 1) f.m = fmaxf(f.m, __shfl_xor_sync(0xFFFFFFFFu, f.m, o));
-#pragma unroll 4
-  for (int s = s0 + way; s <= s1; s += WAYS) {
-    const float* r = row_of(s);
-    f.add(weight(r[kGMaxGroup * D + g], f.m), r[kGMaxGroup * (D + 1) + g], *reinterpret_cast<const float4*>(r + g * D + 4 * col));
+    for (int k = 0; k < 4; ++k) {
+      const float* r = row_of(min(s + k * WAYS, s1));
+      m[k] = s + k * WAYS <= s1 ? r[kGMaxGroup * D + g] : -CUDART_INF_F;
+      l[k] = r[kGMaxGroup * (D + 1) + g];
+      o[k] = *reinterpret_cast<const float4*>(r + g * D + 4 * col);
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) mx = fmaxf(mx, m[k]);
+    const float w = weight(f.m, mx);
+    f.m = mx;
+    f.l *= w; f.o.x *= w; f.o.y *= w; f.o.z *= w; f.o.w *= w;
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      if (s + k * WAYS <= s1) f.add(weight(m[k], mx), l[k], o[k]);
   }
   red[way][col] = f.o;
-  if (col == 0) sums[way] = f.l;
+  if (col == 0) { sums[way] = f.l; refs[way] = f.m; }
   __syncthreads();
   if (way == 0) {
+    Fold r;
+    r.m = -CUDART_INF_F; r.l = 0.f;
+    r.o = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-    for (int w = 1; w < WAYS; ++w) f.add(1.f, sums[w], red[w][col]);
+    for (int w = 0; w < WAYS; ++w) r.m = fmaxf(r.m, refs[w]);
+#pragma unroll
+    for (int w = 0; w < WAYS; ++w) r.add(weight(refs[w], r.m), sums[w], red[w][col]);
     const int64_t h = (int64_t)b * a.Hq + hg / a.NS * a.G + sub * kGMaxGroup + g;
-    f.template write<D>(reinterpret_cast<T*>(a.O) + h * D, a.lse + h, 4 * col);
+    r.template write<D>(reinterpret_cast<T*>(a.O) + h * D, a.lse + h, 4 * col);
   }
+}
+
+// ---- every key of short sequences ---------------------------------------------------------------
+// One block, or a cluster of up to sixteen, per (sequence, KV head, group of 8 heads): a single launch, and nothing to look up before
+// the first copy but the sequence's own position and bounds.  The partial results of a cluster's blocks meet in shared memory.
+constexpr int kSWarps = 8, kSMaxSplit = 16;
+
+template <int D>
+struct ShortLayout {
+  static constexpr int stages = D == 128 ? 2 : 4;
+  static constexpr int ring = kSWarps * stages * Rows<D, kTile>::bytes;
+  static constexpr int merge_off = ring, merge = (kSWarps + 1) * kGMaxGroup * (D + 4) * 4;   // (the last row set: folded)
+  static constexpr int scale_off = merge_off + merge;
+  static constexpr int bar_off = scale_off + kSWarps * stages * kTile * 8;
+  static constexpr int flag_off = bar_off + kSWarps * stages * 8;
+  static constexpr int total = flag_off + 16 + 1024;
+};
+
+template <typename T, int D, int CODE>
+__global__ void __launch_bounds__(kSWarps * 32, 1)
+cache_decode_short_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUtensorMap vmap, CacheDecode a, DamCacheView c) {
+  using LY = ShortLayout<D>;
+  using WS = WarpState<T, D, CODE>;
+  constexpr int STAGES = LY::stages, kThreads = kSWarps * 32, kChunk = kSWarps * kKeys;
+  extern __shared__ unsigned char sm_raw[];
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int blocks = (int)cooperative_groups::this_cluster().num_blocks(), rank = (int)cooperative_groups::this_cluster().block_rank();
+  const int heads = c.Hkv * a.NS, unit = blockIdx.x / blocks, b = unit / heads, hg = unit - b * heads;
+  const int kvh = hg / a.NS, sub = hg - kvh * a.NS, h0 = kvh * a.G + sub * kGMaxGroup, nh = min(kGMaxGroup, a.G - sub * kGMaxGroup);
+  unsigned char* sm = sm_raw + (-sm100::smem_u32(sm_raw) & 1023u);
+  float* mg = reinterpret_cast<float*>(sm + LY::merge_off);
+  const uint32_t base = sm100::smem_u32(sm), ring = base + warp * (STAGES * Rows<D, kTile>::bytes);
+  const uint32_t scales = base + LY::scale_off + warp * (STAGES * kTile * 8), bars = base + LY::bar_off + warp * (STAGES * 8);
+  volatile uint32_t* const gave_up = reinterpret_cast<uint32_t*>(sm + LY::flag_off);
+  if (lane < STAGES) sm100::mbar_init(bars + 8 * lane, 1);
+  if (tid == 0) {
+    *gave_up = 0u;
+    sm100::tma_prefetch_desc(&kmap);
+    sm100::tma_prefetch_desc(&vmap);
+  }
+  sm100::mbar_fence_init();
+  __syncthreads();
+  dam_chain_prologue();
+  const int pos = __ldg(a.pos + b), cu0 = __ldg(c.cu + b), cu1 = __ldg(c.cu + b + 1);
+  const typename WS::Query q = WS::fetch_q(reinterpret_cast<const T*>(a.q) + ((int64_t)b * a.Hq + h0) * D, nh);
+  T* O = reinterpret_cast<T*>(a.O) + ((int64_t)b * a.Hq + h0) * D;
+  float* lse = a.lse + (int64_t)b * a.Hq + h0;
+  const bool bad = (unsigned)pos >= (unsigned)(cu1 - cu0);
+  // this block's chunks of the sequence, and the warp's slice in the first of them
+  const int n = bad ? 0 : pos / kChunk + 1;
+  const Shares sh(n, blocks);
+  const int todo = sh.begin(rank + 1) - sh.begin(rank), key0 = sh.begin(rank) * kChunk + warp * kKeys, len = pos + 1;
+  const float* sp = (lane & 1 ? c.vs : c.ks) + (int64_t)((cu0 >> c.shift) + b) * c.Hkv + kvh;
+  auto issue = [&](int it, int stage) {
+    const int key = key0 + it * kChunk;
+    if (key >= len) return;
+    if (lane < 2 * kTile) {
+      const int at = key + (key + (lane >> 1) * kSlice < len ? (lane >> 1) * kSlice : 0);
+      cp_async4_zfill(scales + 8 * kTile * stage + 4 * lane, sp + (int64_t)(at >> c.shift) * c.Hkv, 4u);
+    }
+    if (sm100::elect_one()) {
+      const uint32_t dst = ring + stage * Rows<D, kTile>::bytes, bar = bars + 8 * stage;
+      sm100::mbar_arrive_expect_tx(bar, Rows<D, kTile>::bytes);
+      sm100::tma_load_3d(dst, &kmap, bar, 0, kvh, cu0 + key);
+      sm100::tma_load_3d(dst + Rows<D, kTile>::v_off, &vmap, bar, 0, kvh, cu0 + key);
+    }
+  };
+#pragma unroll 1
+  for (int s = 0; s < STAGES - 1; ++s) {
+    if (s < todo) issue(s, s);
+    cp_async_commit();
+  }
+  if (blockIdx.x == 0) {
+    // the scratch block for the whole call, its status word included: this block looks at every sequence's position
+    bool any = false;
+    for (int x = tid; x < c.num_seqs; x += kThreads) any |= chunks_of(c, a.pos, x, kChunk) == 0;
+    const int st = __syncthreads_or(any) ? (int)DAM_ERR_INVALID_ARGUMENT : 0;
+    if (tid < 64) a.scratch[tid] = tid == 1 ? (uint32_t)st : 0u;
+  }
+  WS ws;
+  ws.reset();
+  ws.set_q(q, nh, a.scale_log2);
+  int stage = 0, ahead = STAGES - 1;
+  uint32_t phases = 0u;
+  bool lost = false;
+#pragma unroll 1
+  for (int it = 0; it < todo; ++it) {
+    if (it + STAGES - 1 < todo) issue(it + STAGES - 1, ahead);
+    cp_async_commit();
+    cp_async_wait<STAGES - 1>();
+    __syncwarp();
+    const int live = len - (key0 + it * kChunk);
+    if (live > 0 && !lost) {
+      lost = !sm100::mbar_wait(bars + 8 * stage, phases >> stage & 1u, gave_up);
+      phases ^= 1u << stage;
+      const uint32_t rows = ring + stage * Rows<D, kTile>::bytes, sc = scales + 8 * kTile * stage;
+      if (live >= kKeys) ws.template step<WS::kAll, kTile>(rows, sc, 0u);
+      else ws.template step<WS::kFirst, kTile>(rows, sc, (uint32_t)live);
+    }
+    __syncwarp();                                            // the stage is free for the copy the next trip issues
+    stage = stage + 1 == STAGES ? 0 : stage + 1;
+    ahead = ahead + 1 == STAGES ? 0 : ahead + 1;
+  }
+  ws.store(mg + warp * (kGMaxGroup * WS::kRow));
+  __syncthreads();
+  // (a sequence whose position lies outside its capacity has no chunk: O = 0, LSE = -inf)
+  float* folded = mg + kSWarps * kGMaxGroup * WS::kRow;
+  for (int e = 4 * tid; e < nh * D; e += 4 * kThreads) {
+    const int g = e / D, p = e % D;
+    Fold f;
+    f.template warps<kSWarps>(mg + g * WS::kRow, kGMaxGroup * WS::kRow, D, p);
+    if (blocks == 1) {
+      f.template write<D>(O + g * D, lse + g, p);
+    } else {
+      *reinterpret_cast<float4*>(folded + g * WS::kRow + p) = f.o;
+      if (p == 0) { folded[g * WS::kRow + D] = f.m; folded[g * WS::kRow + D + 1] = f.l; }
+    }
+  }
+  if (blocks > 1) fold_cluster<D, kSMaxSplit>(folded, WS::kRow, nh, kThreads, O, lse);
+  sm100::report_expired_wait(gave_up, a.scratch + 1, (uint32_t)DAM_ERR_DEVICE_TIMEOUT);
 }
 
 // ---- the keys of the stored patterns ------------------------------------------------------------
@@ -653,7 +874,7 @@ constexpr int kScales = 2 * kSlice * 4;         // bytes of the scales of a slic
 
 template <int D>
 struct MaskedLayout {
-  static constexpr int ring = kMWarps * kMStages * (Slice<D>::bytes + kScales);
+  static constexpr int ring = kMWarps * kMStages * (Rows<D, 1>::bytes + kScales);
   static constexpr int merge = (kMWarps + 1) * kGMaxGroup * (D + 4) * 4;        // the merge reuses the ring
   static constexpr int codes_off = ring > merge ? ring : merge;                 // u16 per listed key: round-local word * 32 + bit
   static constexpr int words_off = codes_off + kGRoundWords * 32 * 2;           // u32 [head][round-local word]
@@ -704,8 +925,8 @@ cache_decode_masked_kernel(CacheDecode a, DamCacheView c, const unsigned char* _
   const int64_t row0 = (cu0 >> c.shift) + b;
   WS ws;
   ws.reset();
-  ws.load_q(reinterpret_cast<const T*>(a.q) + ((int64_t)b * a.Hq + h0) * D, nh, a.scale_log2);
-  const uint32_t ring = static_cast<uint32_t>(__cvta_generic_to_shared(sm)) + warp * (kMStages * (Slice<D>::bytes + kScales));
+  ws.set_q(WS::fetch_q(reinterpret_cast<const T*>(a.q) + ((int64_t)b * a.Hq + h0) * D, nh), nh, a.scale_log2);
+  const uint32_t ring = static_cast<uint32_t>(__cvta_generic_to_shared(sm)) + warp * (kMStages * (Rows<D, 1>::bytes + kScales));
   const uint64_t stream_policy = l2_evict_first_policy(), keep_policy = l2_evict_last_policy();
   for (int w0 = 0; w0 < nwords; w0 += kGRoundWords) {
     const int total = expand_round<kMWarps>(blob, H, sq, h0, nh, in_window, pos, w0, nwords, codes, whs, warp_tot, keep_policy);
@@ -715,17 +936,17 @@ cache_decode_masked_kernel(CacheDecode a, DamCacheView c, const unsigned char* _
     };
     const int nslices = (total + kSlice - 1) / kSlice, first = split * kMWarps + warp, step = nsplit * kMWarps;
     auto issue = [&](int s, int stage) {
-      const uint32_t dst = ring + stage * (Slice<D>::bytes + kScales);
+      const uint32_t dst = ring + stage * (Rows<D, 1>::bytes + kScales);
 #pragma unroll
-      for (int i = 0; i < kSlice * Slice<D>::pieces / 32; ++i) {
-        const int x = lane + 32 * i, r = x / Slice<D>::pieces, piece = x % Slice<D>::pieces, idx = s * kSlice + r;
+      for (int i = 0; i < kSlice * Rows<D, 1>::pieces / 32; ++i) {
+        const int x = lane + 32 * i, r = x / Rows<D, 1>::pieces, piece = x % Rows<D, 1>::pieces, idx = s * kSlice + r;
         const int j = key_of(codes[idx < total ? idx : s * kSlice]);    // places past the end repeat the slice's first key (not kept below)
-        const uint32_t at = Slice<D>::at(r, piece);
+        const uint32_t at = Rows<D, 1>::at(r, piece);
         cp_async16(dst + at, Kb + (int64_t)j * c.kst + piece * 16, stream_policy);
-        cp_async16(dst + Slice<D>::v_off + at, Vb + (int64_t)j * c.vst + piece * 16, stream_policy);
+        cp_async16(dst + Rows<D, 1>::v_off + at, Vb + (int64_t)j * c.vst + piece * 16, stream_policy);
       }
       const int idx = s * kSlice + (lane & 15), j = key_of(codes[idx < total ? idx : s * kSlice]);
-      cp_async4_zfill(dst + Slice<D>::bytes + 4 * lane, (lane < 16 ? c.ks : c.vs) + (row0 + (j >> c.shift)) * c.Hkv + kvh, 4u);
+      cp_async4_zfill(dst + Rows<D, 1>::bytes + 4 * lane, (lane < 16 ? c.ks : c.vs) + (row0 + (j >> c.shift)) * c.Hkv + kvh, 4u);
     };
 #pragma unroll
     for (int s = 0; s < kMStages - 1; ++s) {
@@ -741,15 +962,15 @@ cache_decode_masked_kernel(CacheDecode a, DamCacheView c, const unsigned char* _
       uint32_t keep = 0u;
 #pragma unroll
       for (int k = 0; k < 2; ++k) {
-        const int idx = s * kSlice + Slice<D>::key(row) + 8 * k;
+        const int idx = s * kSlice + Rows<D, 1>::key(row) + 8 * k;
         if (idx < total) {
           const uint32_t code = codes[idx];
 #pragma unroll
           for (int e = 0; e < 2; ++e) keep |= (whs[(2 * quad + e) * kGRoundWords + (code >> 5)] >> (code & 31u) & 1u) << (2 * k + e);
         }
       }
-      const uint32_t slice = ring + it % kMStages * (Slice<D>::bytes + kScales);
-      ws.template step<WS::kKeep>(slice, slice + Slice<D>::bytes, keep);
+      const uint32_t slice = ring + it % kMStages * (Rows<D, 1>::bytes + kScales);
+      ws.template step<WS::kKeep, 1>(slice, slice + Rows<D, 1>::bytes, keep);
       __syncwarp();                                          // the stage is free for the copy the next trip issues
     }
     cp_async_wait<0>();                                      // (only empty groups are left; the merge reuses the ring)
@@ -772,30 +993,7 @@ cache_decode_masked_kernel(CacheDecode a, DamCacheView c, const unsigned char* _
     }
   }
   if constexpr (CLUSTER) {
-    cooperative_groups::cluster_group cl = cooperative_groups::this_cluster();
-    cl.sync();
-    for (int e = 4 * (split * kThreads + tid); e < nh * D; e += 4 * nsplit * kThreads) {
-      const int g = e / D, p = e % D;
-      float mv[kGMaxSplit], lv[kGMaxSplit];
-      float4 ov[kGMaxSplit];
-      Fold f;
-      f.m = -CUDART_INF_F; f.l = 0.f;
-      f.o = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-      for (int k = 0; k < kGMaxSplit; ++k) {
-        mv[k] = -CUDART_INF_F; lv[k] = 0.f;
-        ov[k] = f.o;
-        if (k < nsplit) {
-          const float* src = cl.map_shared_rank(folded, k) + g * WS::kRow;
-          mv[k] = src[D]; lv[k] = src[D + 1]; ov[k] = *reinterpret_cast<const float4*>(src + p);
-        }
-        f.m = fmaxf(f.m, mv[k]);
-      }
-#pragma unroll
-      for (int k = 0; k < kGMaxSplit; ++k) f.add(weight(mv[k], f.m), lv[k], ov[k]);
-      f.template write<D>(O + g * D, lse + g, p);
-    }
-    cl.sync();                                               // the folded rows stay until every block has read them
+    fold_cluster<D, kGMaxSplit>(folded, WS::kRow, nh, kThreads, O, lse);
   }
 }
 
@@ -808,7 +1006,7 @@ int masked_split(int64_t units, int sm_count) {
 }
 
 // the shared memory a kernel wants, asked for once per device (KEY: a set-up step of its own per instance)
-template <auto KERNEL, int BYTES>
+template <auto KERNEL, int BYTES, bool LARGE_CLUSTER = false>
 cudaError_t opt_in(int key, int* sm_count) {
   int dev = 0;
   DamDeviceInfo di;
@@ -816,15 +1014,29 @@ cudaError_t opt_in(int key, int* sm_count) {
   if (e != cudaSuccess) return e;
   *sm_count = di.sm_count;
   if (di.smem_optin < BYTES) return cudaErrorNotSupported;
-  return dam_device_table().once(dev, key, [](void) -> cudaError_t { return cudaFuncSetAttribute(KERNEL, cudaFuncAttributeMaxDynamicSharedMemorySize, BYTES); });
+  return dam_device_table().once(dev, key, [](void) -> cudaError_t {
+    const cudaError_t r = cudaFuncSetAttribute(KERNEL, cudaFuncAttributeMaxDynamicSharedMemorySize, BYTES);
+    return r != cudaSuccess || !LARGE_CLUSTER ? r : cudaFuncSetAttribute(KERNEL, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+  });
 }
 
 // instance number of <T, D, CODE>
 template <typename T, int D, int CODE> constexpr int kInstance = (sizeof(T) == 4) * 4 + (D == 128) * 2 + CODE;
 
+// Short sequences get a cluster each: of so many blocks that all are resident at once, one per SM (148, 74, 33, 15 and 7 clusters
+// of 1, 2, 4, 8 and 16 blocks: the SMs of a GPC are not a multiple), and no more than have a chunk.  0: there are too many of them.
+int short_split(int64_t units, int64_t longest, int chunk) {
+  static const struct { int split, resident; } sizes[] = {{16, 7}, {8, 15}, {4, 33}, {2, 74}, {1, 148}};
+  for (const auto& s : sizes)
+    if (units <= s.resident && (s.split == 1 || longest > (int64_t)s.split / 2 * chunk)) return s.split;
+  return 0;
+}
+// capacity per block up to which they are short: large clusters leave more SMs without one
+int64_t short_keys(int split) { return split >= 8 ? 1024 : 2048; }
+
 template <typename T, int D, int CODE>
 cudaError_t launch_dense(CacheDecode a, const DamCacheView& c, const dam_cache_t* cache, cudaStream_t st) {
-  constexpr int WARPS = D == 128 ? 12 : 16, STAGES = D == 128 ? 3 : 4;
+  constexpr int WARPS = 8, STAGES = D == 128 ? 3 : 5;
   using LY = DenseLayout<D, WARPS, STAGES>;
   int sms = 0;
   cudaError_t e = opt_in<cache_decode_kernel<T, D, CODE, WARPS, STAGES>, LY::total>(DAM_SETUP_CACHE_SMEM + kInstance<T, D, CODE>, &sms);
@@ -832,26 +1044,43 @@ cudaError_t launch_dense(CacheDecode a, const DamCacheView& c, const dam_cache_t
   const int64_t heads = (int64_t)c.Hkv * a.NS;
   int64_t most = 0, longest = 0;
   for (int b = 0; b < c.num_seqs; ++b) {
-    const int64_t n = ((int64_t)cache->cu_seqlens_host[b + 1] - cache->cu_seqlens_host[b] + LY::chunk - 1) / LY::chunk;
-    most += n;
-    longest = n > longest ? n : longest;
+    const int64_t len = (int64_t)cache->cu_seqlens_host[b + 1] - cache->cu_seqlens_host[b];
+    most += (len + LY::chunk - 1) / LY::chunk;
+    longest = len > longest ? len : longest;
   }
   if (most * heads > 0x7FFFFFFF) return cudaErrorNotSupported;
+  CUtensorMap kmap, vmap;
+  if (!dam_make_tmap_codes(&kmap, c.k, D, c.Hkv, cache->total_tokens, c.kst, c.ksh, kKeys) ||
+      !dam_make_tmap_codes(&vmap, c.v, D, c.Hkv, cache->total_tokens, c.vst, c.vsh, kKeys))
+    return cudaErrorInvalidValue;
+  const int blocks = sms < kMaxShares ? sms : kMaxShares;
+
+  const int64_t units = heads * c.num_seqs;
+  const int split = short_split(units, longest, kSWarps * kKeys);
+  if (split && longest <= split * short_keys(split)) {
+    e = opt_in<cache_decode_short_kernel<T, D, CODE>, ShortLayout<D>::total, true>(DAM_SETUP_CACHE_SMEM + 24 + kInstance<T, D, CODE>, &sms);
+    if (e != cudaSuccess) return e;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(units * split)); cfg.blockDim = dim3(kSWarps * 32); cfg.dynamicSmemBytes = ShortLayout<D>::total; cfg.stream = st;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = (unsigned)split; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr; cfg.numAttrs = 2;
+    return cudaLaunchKernelEx(&cfg, cache_decode_short_kernel<T, D, CODE>, kmap, vmap, a, c);
+  }
+
   // all heads side by side where that leaves no more than an eighth of the SMs without work; and no more shares than there can be
   // chunks
-  const int blocks = sms < kMaxShares ? sms : kMaxShares;
   a.side = heads > 1 && heads <= blocks && blocks % heads * 8 <= blocks ? (int)heads : 1;
   int64_t shares = blocks / a.side;
   const int64_t list = a.side > 1 ? most : most * heads;
   if (list < shares) shares = list > 0 ? list : 1;
-  CUtensorMap kmap, vmap;
-  if (!dam_make_tmap_codes(&kmap, c.k, D, c.Hkv, cache->total_tokens, c.kst, c.ksh, kSlice) ||
-      !dam_make_tmap_codes(&vmap, c.v, D, c.Hkv, cache->total_tokens, c.vst, c.vsh, kSlice))
-    return cudaErrorInvalidValue;
   float* partial = reinterpret_cast<float*>(a.scratch + 64);
   e = dam_launch_chained(cache_decode_kernel<T, D, CODE, WARPS, STAGES>, dim3((unsigned)(shares * a.side)), dim3(WARPS * 32), LY::total, st, kmap,
                          vmap, a, c, partial);
-  if (e != cudaSuccess || shares == 1 || longest <= 1) return e;   // (then every sequence is whole in one block)
+  if (e != cudaSuccess || shares == 1 || longest <= LY::chunk) return e;   // (then every sequence is whole in one block)
   const int64_t grid = heads * (a.G < kGMaxGroup ? a.G : kGMaxGroup) * c.num_seqs;
   if (grid > 0x7FFFFFFF) return cudaErrorNotSupported;
   return dam_launch_chained(cache_join_kernel<T, D>, dim3((unsigned)grid), dim3(256), 0, st, a, c, (const float*)partial, LY::chunk, (int)shares);
