@@ -1036,7 +1036,7 @@ int64_t short_keys(int split) { return split >= 8 ? 1024 : 2048; }
 
 template <typename T, int D, int CODE>
 cudaError_t launch_dense(CacheDecode a, const DamCacheView& c, const dam_cache_t* cache, cudaStream_t st) {
-  constexpr int WARPS = 8, STAGES = D == 128 ? 3 : 5;
+  constexpr int WARPS = D == 128 ? 8 : 16, STAGES = D == 128 ? 3 : 2;
   using LY = DenseLayout<D, WARPS, STAGES>;
   int sms = 0;
   cudaError_t e = opt_in<cache_decode_kernel<T, D, CODE, WARPS, STAGES>, LY::total>(DAM_SETUP_CACHE_SMEM + kInstance<T, D, CODE>, &sms);
