@@ -7,6 +7,7 @@ fails, an exception is raised.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 from dataclasses import dataclass
 from typing import List, Optional, Sequence
@@ -141,7 +142,7 @@ class Shape:
     cu_dev: Optional[torch.Tensor]
     lengths: List[int]
 
-    @property
+    @functools.cached_property
     def ref(self):
         return ctypes.byref(self.c)
 
@@ -362,8 +363,10 @@ class Cache:
     v_codes: Optional[torch.Tensor]
     k_scales: Optional[torch.Tensor]
     v_scales: Optional[torch.Tensor]
+    num_seqs: int                # (as in c; a field of a ctypes structure takes several times as long to read)
+    head_dim: int
 
-    @property
+    @functools.cached_property
     def ref(self):
         return ctypes.byref(self.c)
 
@@ -400,7 +403,7 @@ def make_cache(cu_seqlens: Sequence[int], Hkv: int, d: int, code: str = "int8", 
         (c.k_codes, c.v_codes), (c.k_scales, c.v_scales) = map(_ptr, codes), map(_ptr, scales)
     (c.k_stride_tok, c.k_stride_head), (c.v_stride_tok, c.v_stride_head) = (
         (Hkv * d, d) if x is None or x.numel() == 0 else (x.stride(0), x.stride(1)) for x in codes)
-    return Cache(c, cu_host, cu_dev, lengths, *codes, *scales)
+    return Cache(c, cu_host, cu_dev, lengths, *codes, *scales, len(lengths), d)
 
 
 def dam_cache_sizes(cache: Cache, Hq: int):
@@ -410,20 +413,23 @@ def dam_cache_sizes(cache: Cache, Hq: int):
     return rows.value, scratch.value
 
 
-def _check_starts(starts: Optional[torch.Tensor], cache: Cache):
-    if starts is not None:
-        assert starts.dtype == torch.int32 and starts.numel() == cache.c.num_seqs and starts.is_contiguous()
+def _per_sequence(x: torch.Tensor, n: int) -> int:
+    """Pointer of an int32 tensor with one element per sequence."""
+    assert x.dtype is torch.int32 and x.numel() == n and x.is_contiguous()
+    return x.data_ptr()
 
 
 def dam_cache_write(K: torch.Tensor, V: torch.Tensor, tokens: Shape, cache: Cache, starts: Optional[torch.Tensor] = None,
                     scratch: Optional[torch.Tensor] = None) -> torch.Tensor:
     """Quantises the packed rows K, V (`tokens` says how many each sequence gets) into the cache, from token starts[b] of
     sequence b on (int32 on the device; None: token 0).  Returns scratch."""
-    _check_starts(starts, cache)
+    device = K.device
     if scratch is None:
-        scratch = _alloc(256, K.device)
-    rc = lib().dam_cache_write(_ptr(K), _ptr(V), tokens.ref, _ptr(starts), cache.ref, _ptr(scratch), scratch.numel(), _stream(K.device))
-    _check(rc, "dam_cache_write")
+        scratch = _alloc(256, device)
+    rc = lib().dam_cache_write(K.data_ptr(), V.data_ptr(), tokens.ref, None if starts is None else _per_sequence(starts, cache.num_seqs),
+                               cache.ref, scratch.data_ptr(), scratch.numel(), _stream(device))
+    if rc:
+        _check(rc, "dam_cache_write")
     return scratch
 
 
@@ -431,7 +437,6 @@ def dam_cache_read(cache: Cache, tokens: Shape, starts: Optional[torch.Tensor] =
                    V: Optional[torch.Tensor] = None, scratch: Optional[torch.Tensor] = None):
     """Reads tokens starts[b] ... of every sequence back, as packed rows (`tokens` says how many, of which type and strides).
     Returns (K, V, scratch)."""
-    _check_starts(starts, cache)
     device = cache.k_codes.device
     if K is None or V is None:
         s = tokens.c
@@ -441,8 +446,10 @@ def dam_cache_read(cache: Cache, tokens: Shape, starts: Optional[torch.Tensor] =
         K, V = K if K is not None else rows[0], V if V is not None else rows[1]
     if scratch is None:
         scratch = _alloc(256, device)
-    rc = lib().dam_cache_read(cache.ref, tokens.ref, _ptr(starts), _ptr(K), _ptr(V), _ptr(scratch), scratch.numel(), _stream(device))
-    _check(rc, "dam_cache_read")
+    rc = lib().dam_cache_read(cache.ref, tokens.ref, None if starts is None else _per_sequence(starts, cache.num_seqs), K.data_ptr(),
+                              V.data_ptr(), scratch.data_ptr(), scratch.numel(), _stream(device))
+    if rc:
+        _check(rc, "dam_cache_read")
     return K, V, scratch
 
 
@@ -451,19 +458,20 @@ def dam_cache_decode_attention(q: torch.Tensor, cache: Cache, positions: torch.T
                                lse: Optional[torch.Tensor] = None, scratch: Optional[torch.Tensor] = None):
     """One new token per sequence against an 8-bit cache (q, O: [B, Hq, d]; positions int32 [B]): every key up to its position,
     or, with a mask blob, those that its patterns keep.  Returns (O, LSE [B, Hq] fp32, scratch)."""
-    B, Hq = cache.c.num_seqs, q.shape[1]
-    assert q.is_contiguous() and q.shape == (B, Hq, cache.c.head_dim)
-    assert positions.dtype == torch.int32 and positions.numel() == B and positions.is_contiguous()
+    n, Hq, _ = shape = q.shape
+    dtype, device = q.dtype, q.device
+    assert shape == (cache.num_seqs, Hq, cache.head_dim) and q.is_contiguous() and (dtype is torch.bfloat16 or dtype is torch.float32)
     if O is None:
         O = torch.empty_like(q)
     if lse is None:
-        lse = torch.empty(B, Hq, dtype=torch.float32, device=q.device)
+        lse = torch.empty(n, Hq, dtype=torch.float32, device=device)
     if scratch is None:
-        scratch = _alloc(dam_cache_sizes(cache, Hq)[1], q.device)
-    rc = lib().dam_cache_decode_attention(_ptr(q), cache.ref, _ptr(mask), _ptr(positions), Hq,
-                                          DAM_BF16 if q.dtype == torch.bfloat16 else DAM_F32, softmax_scale, _ptr(O),
-                                          _ptr(lse), _ptr(scratch), scratch.numel(), _stream(q.device))
-    _check(rc, "dam_cache_decode_attention")
+        scratch = _alloc(dam_cache_sizes(cache, Hq)[1], device)
+    rc = lib().dam_cache_decode_attention(q.data_ptr(), cache.ref, None if mask is None else mask.data_ptr(), _per_sequence(positions, n), Hq,
+                                          DAM_BF16 if dtype is torch.bfloat16 else DAM_F32, softmax_scale, O.data_ptr(), lse.data_ptr(),
+                                          scratch.data_ptr(), scratch.numel(), _stream(device))
+    if rc:
+        _check(rc, "dam_cache_decode_attention")
     return O, lse, scratch
 
 

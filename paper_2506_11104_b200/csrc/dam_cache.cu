@@ -184,8 +184,9 @@ struct WriteSlot {
   __device__ __forceinline__ void go_on() { x += dx; codes += dc; scale += ds; }
 };
 
-// PASSES: rows of a block of tokens that a thread holds 8 elements of.  The rows of the next slot are on their way while this
-// one's are quantised.
+// PASSES: rows of a block of tokens that a thread holds 8 elements of.  Enough blocks of threads share an SM that some wait for their
+// rows while others quantise theirs (a prompt of 128k tokens 133 us; with the next slot's rows requested ahead, at twice the
+// registers and four blocks, 160).
 template <typename T, int D, int CODE, int THREADS, int PASSES, int BLOCKS>
 __global__ void __launch_bounds__(THREADS, BLOCKS)
 cache_write_kernel(CacheRows src, const int32_t* __restrict__ starts, DamCacheView c, uint32_t slots, uint32_t* __restrict__ scratch) {
@@ -196,8 +197,8 @@ cache_write_kernel(CacheRows src, const int32_t* __restrict__ starts, DamCacheVi
   const int tid = threadIdx.x, r0 = tid / TPR;
   constexpr int whole = PASSES * RPP;                        // = block_tokens
   Slots<WriteSlot<T, D>> it(c);
-  Eight<T> v[PASSES], w[PASSES];
-  float before = 0.f, before_next = 0.f;
+  Eight<T> v[PASSES];
+  float before = 0.f;
   auto load = [&](const WriteSlot<T, D>& y, Eight<T>* r, float& b) {
     if (y.first == 0 && y.last == whole) {
 #pragma unroll
@@ -212,16 +213,13 @@ cache_write_kernel(CacheRows src, const int32_t* __restrict__ starts, DamCacheVi
     }
   };
   bool have = it.seek(c, src, starts, slots);
-  if (have) load(it.at, v, before);
   int turn = 0;
   while (have) {
-    // this slot's, while the cursor goes on
+    load(it.at, v, before);
     unsigned char* const codes = it.at.codes;
     float* const scale = it.at.scale;
     const int64_t cst = it.at.cst;
     const int first = it.at.first, last = it.at.last;
-    have = it.next(c, src, starts, slots);
-    if (have) load(it.at, w, before_next);
     uint32_t top = 0u;
 #pragma unroll
     for (int i = 0; i < PASSES; ++i) v[i].top(top);
@@ -261,9 +259,7 @@ cache_write_kernel(CacheRows src, const int32_t* __restrict__ starts, DamCacheVi
         if (r >= first) *reinterpret_cast<uint2*>(codes + (int64_t)(r - r0) * cst) = make_uint2(0u, 0u);
     }
     if (tid == 0) *scale = s;
-    before = before_next; turn ^= 1;
-#pragma unroll
-    for (int i = 0; i < PASSES; ++i) v[i] = w[i];
+    turn ^= 1; have = it.next(c, src, starts, slots);
   }
 }
 
@@ -400,21 +396,22 @@ CacheRows rows_of(const void* K, const void* V, const dam_shape_t* t) {
 
 template <int N> using Int = std::integral_constant<int, N>;
 
-// Threads, rows per thread and blocks per SM of a write, by the elements of a block of tokens.
+// Threads, rows per thread and blocks per SM of a write, by the elements of a block of tokens: 8 rows per thread (fp32: 4) keep what
+// a slot costs beside its rows small.
 template <typename T, int D, typename F>
 cudaError_t write_form(int block_tokens, F go) {
   const int rows = block_tokens * (D / 64);                  // (of 64 elements)
   if constexpr (sizeof(T) == 2) {
     if (rows <= 16) return go(Int<128>(), Int<1>(), Int<8>());
     if (rows == 32) return go(Int<128>(), Int<2>(), Int<8>());
-    if (rows == 64) return go(Int<128>(), Int<4>(), Int<6>());
-    if (rows == 128) return go(Int<128>(), Int<8>(), Int<4>());
-    if constexpr (D == 128) return go(Int<256>(), Int<8>(), Int<2>());
+    if (rows == 64) return go(Int<128>(), Int<4>(), Int<8>());
+    if (rows == 128) return go(Int<128>(), Int<8>(), Int<7>());
+    if constexpr (D == 128) return go(Int<256>(), Int<8>(), Int<3>());
   } else {
     if (rows <= 16) return go(Int<128>(), Int<1>(), Int<8>());
-    if (rows == 32) return go(Int<128>(), Int<2>(), Int<6>());
-    if (rows == 64) return go(Int<128>(), Int<4>(), Int<4>());
-    if (rows == 128) return go(Int<256>(), Int<4>(), Int<2>());
+    if (rows == 32) return go(Int<128>(), Int<2>(), Int<8>());
+    if (rows == 64) return go(Int<128>(), Int<4>(), Int<7>());
+    if (rows == 128) return go(Int<256>(), Int<4>(), Int<3>());
     if constexpr (D == 128) return go(Int<512>(), Int<4>(), Int<1>());
   }
   return cudaErrorNotSupported;
@@ -434,7 +431,6 @@ cudaError_t launch_write(const CacheRows& src, const int32_t* starts, const DamC
     return dam_launch_chained(cache_write_one_kernel<T, D, CODE>, dim3((unsigned)((rows + 3) / 4)), dim3(128), 0, st, src, starts, c,
                               (uint32_t)rows, scratch);
   }
-  // 8 rows per thread (fp32: 4) of blocks of 128 threads keep what a slot costs beside its rows small, and still leave 4 blocks per SM
   auto go = [&](auto threads, auto passes, auto blocks) {
     constexpr int THREADS = decltype(threads)::value, PASSES = decltype(passes)::value, BLOCKS = decltype(blocks)::value;
     return dam_launch_chained(cache_write_kernel<T, D, CODE, THREADS, PASSES, BLOCKS>, dim3(slot_grid(slots, c, sms * BLOCKS)), dim3(THREADS),

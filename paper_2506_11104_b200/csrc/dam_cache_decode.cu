@@ -20,13 +20,49 @@
 #include <math_constants.h>
 
 #include "dam_cache.cuh"
-#include "dam_decode_common.cuh"
 #include "sm100_ptx.cuh"
 
 namespace {
 
 constexpr int kSlice = 16;             // keys of a slice: the rows of the first instruction, the k side of the second
 constexpr int kTile = 2;               // slices that a warp takes at a time where the keys are contiguous: two independent chains
+
+constexpr int kGMaxGroup = 8;         // query heads a block takes: the narrow side of the instructions' tiles
+
+__device__ __forceinline__ float g_ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+// K / V rows are read once per launch: they are marked to leave L2 first, so that the few lines every launch reads
+// again (blob header, sequence records, pattern words, queries) are still there next time
+__device__ __forceinline__ uint64_t l2_evict_first_policy() {
+  uint64_t p;
+  asm volatile("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(p));
+  return p;
+}
+__device__ __forceinline__ uint64_t l2_evict_last_policy() {
+  uint64_t p;
+  asm volatile("createpolicy.fractional.L2::evict_last.b64 %0, 1.0;" : "=l"(p));
+  return p;
+}
+__device__ __forceinline__ uint32_t ldg_keep(const uint32_t* ptr, uint64_t policy) {
+  uint32_t v;
+  asm volatile("ld.global.nc.L2::cache_hint.u32 %0, [%1], %2;" : "=r"(v) : "l"(ptr), "l"(policy));
+  return v;
+}
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, uint64_t policy) {
+  asm volatile("cp.async.cg.shared.global.L2::cache_hint [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "l"(policy) : "memory");
+}
+__device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+// transpose of an 8 x 8 matrix of 16-bit elements held one row pair per lane (the accumulator layout of two columns)
+__device__ __forceinline__ uint32_t movmatrix_trans(uint32_t a) {
+  uint32_t d;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(d) : "r"(a));
+  return d;
+}
 
 __device__ __forceinline__ void cp_async16_zfill(uint32_t dst, const void* src, uint32_t bytes) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
@@ -872,6 +908,84 @@ cache_decode_short_kernel(const __grid_constant__ CUtensorMap kmap, const __grid
 constexpr int kMWarps = 5, kMStages = 2, kMBlocks = 4;
 constexpr int kScales = 2 * kSlice * 4;         // bytes of the scales of a slice
 
+constexpr int kGRoundWords = 128;     // pattern words expanded per round (at most 4096 keys)
+constexpr int kGMaxSplit = 8;         // blocks of a cluster (the largest portable size)
+
+// One round of the key list of `G` heads (h0, h0 + 1, ...): kGRoundWords pattern words from word w0 on, a thread per word, the
+// words of all heads OR-ed.  A listed key is stored as (word, bit) of the round in `codes`; which heads keep it is read back
+// from the round's words in `whs`, [head][word].  By all threads of the block (WARPS warps, at least kGRoundWords threads);
+// returns the number of listed keys.
+template <int WARPS>
+__device__ __forceinline__ int expand_round(const unsigned char* blob, const DamHeader* H, const DamSeq& sq, int h0, int G, bool in_window,
+                                            int pos, int w0, int nwords, unsigned short* codes, uint32_t* whs, int* warp_tot,
+                                            uint64_t keep_policy) {
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, W = sq.W;
+  const int wi = w0 + tid;
+  const bool mine = tid < kGRoundWords && wi < nwords;    // (threads beyond the round's words hold no word)
+  // The words of all heads are requested before any is looked at: one trip to memory, not one per head.  Below the window, word
+  // wi >= W holds diagonals: diagonal r = 32 (wi - W) + k selects key pos - r; dropped when that key is a matched column of the head
+  // (then it is in the list already): bit k of the reversed 32-bit window of V that ends at key pos - 32 (wi - W).
+  const bool diagonals = mine && !in_window && wi >= W;
+  const DamHeadBits hb = dam_head_bits(blob, H, sq, h0);
+  const uint32_t* word = in_window ? hb.M + (size_t)pos * W + wi : wi < W ? hb.V + wi : hb.D + (wi - W);
+  const int64_t per_head = in_window ? (int64_t)sq.L * W : 3ll * W;
+  const int x = pos - 32 * (wi - W) - 31, xw = x >> 5;
+  uint32_t wh[kGMaxGroup], uni = 0u;
+#pragma unroll
+  for (int g0 = 0; g0 < kGMaxGroup; g0 += 4) {            // (four heads at a time: most groups have no more)
+    uint32_t lo[4], hi[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int g = g0 + i;
+      wh[g] = lo[i] = hi[i] = 0u;
+      if (g0 < G) {
+        if (mine && g < G) wh[g] = ldg_keep(word + g * per_head, keep_policy);
+        if (diagonals && g < G && xw >= 0 && xw < W) lo[i] = ldg_keep(hb.V + 3ll * W * g + xw, keep_policy);
+        if (diagonals && g < G && xw + 1 >= 0 && xw + 1 < W) hi[i] = ldg_keep(hb.V + 3ll * W * g + xw + 1, keep_policy);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      wh[g0 + i] &= ~__brev(__funnelshift_r(lo[i], hi[i], x & 31));
+      uni |= wh[g0 + i];
+    }
+  }
+  const int cnt = __popc(uni);
+  int off = cnt;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int y = __shfl_up_sync(0xFFFFFFFFu, off, o);
+    if (lane >= o) off += y;
+  }
+  __syncthreads();                                        // the previous round's list is no longer read
+  if (lane == 31) warp_tot[warp] = off;
+  if (tid < kGRoundWords) {
+#pragma unroll
+    for (int g = 0; g < kGMaxGroup; ++g) whs[g * kGRoundWords + tid] = wh[g];
+  }
+  __syncthreads();
+  int total = 0, before = 0;
+#pragma unroll
+  for (int w = 0; w < WARPS; ++w) {
+    const int wt = warp_tot[w];
+    if (w < warp) before += wt;
+    total += wt;
+  }
+  // the words are spread to the warps, a lane per bit (a thread that took its own word's bits one by one needed up to 32 steps, and
+  // the words of a band are full)
+  __shared__ uint2 listed[kGRoundWords];
+  if (tid < kGRoundWords) listed[tid] = make_uint2(uni, (uint32_t)(off + before - cnt));
+  __syncthreads();
+  const int used = min(kGRoundWords, nwords - w0);
+#pragma unroll 4
+  for (int w = warp; w < used; w += WARPS) {
+    const uint2 l = listed[w];
+    if (l.x >> lane & 1u) codes[l.y + __popc(l.x & ((1u << lane) - 1u))] = (unsigned short)(w * 32 + lane);
+  }
+  __syncthreads();
+  return total;
+}
+
 template <int D>
 struct MaskedLayout {
   static constexpr int ring = kMWarps * kMStages * (Rows<D, 1>::bytes + kScales);
@@ -898,7 +1012,9 @@ cache_decode_masked_kernel(CacheDecode a, DamCacheView c, const unsigned char* _
   const int kvh = hg / a.NS, sub = hg % a.NS, h0 = kvh * a.G + sub * kGMaxGroup, nh = min(kGMaxGroup, a.G - sub * kGMaxGroup);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, row = lane >> 2, quad = lane & 3;
   const DamHeader* H = reinterpret_cast<const DamHeader*>(blob);
+  // (the header, the position, the bounds and the queries are requested together: one round trip to memory)
   const int pos = __ldg(a.pos + b), cu0 = __ldg(c.cu + b), cu1 = __ldg(c.cu + b + 1);
+  const typename WS::Query q = WS::fetch_q(reinterpret_cast<const T*>(a.q) + ((int64_t)b * a.Hq + h0) * D, nh);
   const bool bad_blob = H->magic != DAM_MAGIC || H->num_seqs != c.num_seqs || H->num_q_heads != a.Hq;
   const bool bad = bad_blob || pos < 0 || pos >= cu1 - cu0;
   T* O = reinterpret_cast<T*>(a.O) + ((int64_t)b * a.Hq + h0) * D;
@@ -925,7 +1041,7 @@ cache_decode_masked_kernel(CacheDecode a, DamCacheView c, const unsigned char* _
   const int64_t row0 = (cu0 >> c.shift) + b;
   WS ws;
   ws.reset();
-  ws.set_q(WS::fetch_q(reinterpret_cast<const T*>(a.q) + ((int64_t)b * a.Hq + h0) * D, nh), nh, a.scale_log2);
+  ws.set_q(q, nh, a.scale_log2);
   const uint32_t ring = static_cast<uint32_t>(__cvta_generic_to_shared(sm)) + warp * (kMStages * (Rows<D, 1>::bytes + kScales));
   const uint64_t stream_policy = l2_evict_first_policy(), keep_policy = l2_evict_last_policy();
   for (int w0 = 0; w0 < nwords; w0 += kGRoundWords) {

@@ -20,7 +20,7 @@
 #include <cuda_bf16.h>
 #include <math_constants.h>
 
-#include "dam_decode_common.cuh"
+#include "dam_internal.cuh"
 
 namespace {
 
@@ -29,7 +29,45 @@ constexpr int kGStages = 1;           // chunks of 16 keys a warp holds in share
                                       // the other 15 warps of the SM cover the wait (measured faster than 2 stages at half the occupancy)
 constexpr int kGMinBlocks = 4;         // resident blocks per SM the register limit is sized for
 constexpr int kGChunk = 16;           // keys per chunk (the K dimension of the P V instruction)
+constexpr int kGRoundWords = 128;     // pattern words expanded per round (at most 4096 keys)
+constexpr int kGMaxSplit = 8;         // blocks of a cluster (the largest portable size)
+constexpr int kGMaxGroup = 8;         // query heads per KV head this kernel takes (rows 0..7 of the m16 tile)
 
+__device__ __forceinline__ float g_ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+// K / V rows are read once per launch: they are marked to leave L2 first, so that the few lines every launch reads
+// again (blob header, sequence records, pattern words, queries) are still there next time
+__device__ __forceinline__ uint64_t l2_evict_first_policy() {
+  uint64_t p;
+  asm volatile("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(p));
+  return p;
+}
+__device__ __forceinline__ uint64_t l2_evict_last_policy() {
+  uint64_t p;
+  asm volatile("createpolicy.fractional.L2::evict_last.b64 %0, 1.0;" : "=l"(p));
+  return p;
+}
+__device__ __forceinline__ uint32_t ldg_keep(const uint32_t* ptr, uint64_t policy) {
+  uint32_t v;
+  asm volatile("ld.global.nc.L2::cache_hint.u32 %0, [%1], %2;" : "=r"(v) : "l"(ptr), "l"(policy));
+  return v;
+}
+// bits [x, x + 32) of a bit array of nwords words, zero outside it (x may be negative)
+__device__ __forceinline__ uint32_t window32_keep(const uint32_t* bits, int nwords, int x, uint64_t policy) {
+  const int w = x >> 5, sh = x & 31;
+  const uint32_t lo = (w >= 0 && w < nwords) ? ldg_keep(bits + w, policy) : 0u;
+  const uint32_t hi = (w + 1 >= 0 && w + 1 < nwords) ? ldg_keep(bits + w + 1, policy) : 0u;
+  return __funnelshift_r(lo, hi, sh);
+}
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, uint64_t policy) {
+  asm volatile("cp.async.cg.shared.global.L2::cache_hint [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "l"(policy) : "memory");
+}
+__device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 __device__ __forceinline__ void ldmatrix_x4(uint32_t addr, uint32_t* r) {
   asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];"
                : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr));
@@ -43,6 +81,13 @@ __device__ __forceinline__ void mma_16816(float* c, const uint32_t* a, uint32_t 
   asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
+// transpose of an 8 x 8 matrix of 16-bit elements held one row pair per lane (the accumulator layout of two columns)
+__device__ __forceinline__ uint32_t movmatrix_trans(uint32_t a) {
+  uint32_t d;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(d) : "r"(a));
+  return d;
+}
+
 template <int D>
 struct GLayout {
   static constexpr int row_bytes = D * 2;
@@ -128,8 +173,56 @@ decode_group_kernel(const __nv_bfloat16* __restrict__ q, const __nv_bfloat16* __
   const uint32_t stage0 = static_cast<uint32_t>(__cvta_generic_to_shared(gsm)) + warp * (kGStages * LY::stage_bytes);
   const uint64_t stream_policy = l2_evict_first_policy(), keep_policy = l2_evict_last_policy();
   for (int w0 = 0; w0 < nwords; w0 += kGRoundWords) {
-    // ---- one key list for the whole group
-    const int total = expand_round<kGWarps>(blob, H, sq, h0, G, in_window, pos, w0, nwords, codes, whs, warp_tot, keep_policy);
+    // ---- one key list for the whole group: a thread per pattern word, the words of all heads OR-ed.  A listed key
+    //      is stored as (word, bit) of the round; which heads keep it is read back from the round's words
+    const int wi = w0 + tid;                                // (threads beyond the round's words hold no word)
+    uint32_t wh[kGMaxGroup], uni = 0u;
+#pragma unroll
+    for (int g = 0; g < kGMaxGroup; ++g) {
+      wh[g] = 0u;
+      if (g < G && tid < kGRoundWords && wi < nwords) {
+        const DamHeadBits hb = dam_head_bits(blob, H, sq, h0 + g);
+        if (in_window) {
+          wh[g] = ldg_keep(hb.M + (size_t)pos * W + wi, keep_policy);
+        } else if (wi < W) {
+          wh[g] = ldg_keep(hb.V + wi, keep_policy);
+        } else {
+          // diagonal r = 32 (wi - W) + k selects key pos - r; dropped when that key is a matched column of the head
+          // (then it is in the list already): bit k of the reversed 32-bit window of V that ends at key pos - 32 (wi - W)
+          const int r0 = 32 * (wi - W);
+          wh[g] = ldg_keep(hb.D + (wi - W), keep_policy) & ~__brev(window32_keep(hb.V, W, pos - r0 - 31, keep_policy));
+        }
+        uni |= wh[g];
+      }
+    }
+    const int cnt = __popc(uni);
+    int off = cnt;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int y = __shfl_up_sync(0xFFFFFFFFu, off, o);
+      if (lane >= o) off += y;
+    }
+    __syncthreads();                                        // the previous round's list is no longer read
+    if (lane == 31) warp_tot[warp] = off;
+    if (tid < kGRoundWords) {
+#pragma unroll
+      for (int g = 0; g < kGMaxGroup; ++g) whs[g * kGRoundWords + tid] = wh[g];
+    }
+    __syncthreads();
+    int total = 0, before = 0;
+#pragma unroll
+    for (int w = 0; w < kGWarps; ++w) {
+      const int wt = warp_tot[w];
+      if (w < warp) before += wt;
+      total += wt;
+    }
+    off += before - cnt;
+    while (uni) {
+      const int k = __ffs(uni) - 1;
+      uni &= uni - 1u;
+      codes[off++] = (unsigned short)(tid * 32 + k);
+    }
+    __syncthreads();
     // key index of a listed key
     auto key_of = [&](uint32_t code) -> int {
       const int w = w0 + (int)(code >> 5), k = (int)(code & 31u);
