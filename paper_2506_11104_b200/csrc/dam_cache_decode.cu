@@ -416,35 +416,45 @@ struct Fold {
   }
 };
 
-// The folded rows ([head][stride]: O, reference, sum) of the blocks of a cluster, at most MOST of them, to the result.
-template <int D, int MOST, typename T>
-__device__ __forceinline__ void fold_cluster(float* folded, int stride, int heads, int threads, T* O, float* lse) {
-  cooperative_groups::cluster_group cl = cooperative_groups::this_cluster();
-  const int blocks = (int)cl.num_blocks(), rank = (int)cl.block_rank();
-  cl.sync();
-  for (int e = 4 * (rank * threads + (int)threadIdx.x); e < heads * D; e += 4 * blocks * threads) {
-    const int g = e / D, p = e % D;
-    float mv[MOST], lv[MOST];
-    float4 ov[MOST];
-    Fold f;
-    f.m = -CUDART_INF_F; f.l = 0.f;
-    f.o = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-    for (int k = 0; k < MOST; ++k) {
-      mv[k] = -CUDART_INF_F; lv[k] = 0.f;
-      ov[k] = f.o;
-      if (k < blocks) {
-        const float* src = cl.map_shared_rank(folded, k) + g * stride;
-        mv[k] = src[D]; lv[k] = src[D + 1]; ov[k] = *reinterpret_cast<const float4*>(src + p);
-      }
-      f.m = fmaxf(f.m, mv[k]);
+// The blocks of a cluster join their results by pushing: element e of the `heads` rows belongs to block e / part; every block folds
+// its warps' rows and stores them, and their references and sums, into the shared memory of the blocks they belong to, and after one
+// barrier every block has what it needs.  (Blocks that pulled needed a second barrier, and waited for remote reads between the two.)
+struct ClusterJoin {
+  static constexpr int most = 16, bytes = kGMaxGroup * 128 * 4 + most * kGMaxGroup * 8;
+  float* rows;                         // [block][part]
+  float2* refs;                        // [block][head]: reference and sum
+  __device__ __forceinline__ explicit ClusterJoin(unsigned char* at)
+      : rows(reinterpret_cast<float*>(at)), refs(reinterpret_cast<float2*>(at + kGMaxGroup * 128 * 4)) {}
+  // a first barrier, early: every block has begun before any is written to
+  static __device__ __forceinline__ void begin() { asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory"); }
+  template <int D, int WARPS, typename T>
+  __device__ __forceinline__ void join(const float* mg, int stride, int heads, T* O, float* lse) const {
+    cooperative_groups::cluster_group cl = cooperative_groups::this_cluster();
+    const int blocks = (int)cl.num_blocks(), rank = (int)cl.block_rank(), part = heads * D / blocks;
+    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+    for (int e = 4 * threadIdx.x; e < heads * D; e += 4 * blockDim.x) {
+      const int g = e / D, p = e % D, to = e / part, first = to * part;
+      Fold f;
+      f.template warps<WARPS>(mg + g * stride, kGMaxGroup * stride, D, p);
+      *reinterpret_cast<float4*>(cl.map_shared_rank(rows, to) + rank * part + e - first) = f.o;
+      if (p == 0 || e == first) cl.map_shared_rank(refs, to)[rank * kGMaxGroup + g] = make_float2(f.m, f.l);
     }
-#pragma unroll
-    for (int k = 0; k < MOST; ++k) f.add(weight(mv[k], f.m), lv[k], ov[k]);
-    f.template write<D>(O + g * D, lse + g, p);
+    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+    for (int i = 4 * threadIdx.x; i < part; i += 4 * blockDim.x) {
+      const int e = rank * part + i, g = e / D;
+      Fold f;
+      f.m = -CUDART_INF_F; f.l = 0.f;
+      f.o = make_float4(0.f, 0.f, 0.f, 0.f);
+      for (int k = 0; k < blocks; ++k) f.m = fmaxf(f.m, refs[k * kGMaxGroup + g].x);
+      for (int k = 0; k < blocks; ++k) {
+        const float2 r = refs[k * kGMaxGroup + g];
+        f.add(weight(r.x, f.m), r.y, *reinterpret_cast<const float4*>(rows + k * part + i));
+      }
+      f.template write<D>(O + g * D, lse + g, e % D);
+    }
   }
-  cl.sync();                                                 // the folded rows stay until every block has read them
-}
+};
 
 struct CacheDecode {
   const void* q;
@@ -785,14 +795,14 @@ cache_join_kernel(CacheDecode a, DamCacheView c, const float* __restrict__ parti
 // ---- every key of short sequences ---------------------------------------------------------------
 // One block, or a cluster of up to sixteen, per (sequence, KV head, group of 8 heads): a single launch, and nothing to look up before
 // the first copy but the sequence's own position and bounds.  The partial results of a cluster's blocks meet in shared memory.
-constexpr int kSWarps = 8, kSMaxSplit = 16;
+constexpr int kSWarps = 8;
 
 template <int D>
 struct ShortLayout {
   static constexpr int stages = D == 128 ? 2 : 4;
   static constexpr int ring = kSWarps * stages * Rows<D, kTile>::bytes;
-  static constexpr int merge_off = ring, merge = (kSWarps + 1) * kGMaxGroup * (D + 4) * 4;   // (the last row set: folded)
-  static constexpr int scale_off = merge_off + merge;
+  static constexpr int merge_off = ring, merge = kSWarps * kGMaxGroup * (D + 4) * 4;
+  static constexpr int join_off = merge_off + merge, scale_off = join_off + ClusterJoin::bytes;
   static constexpr int bar_off = scale_off + kSWarps * stages * kTile * 8;
   static constexpr int flag_off = bar_off + kSWarps * stages * 8;
   static constexpr int total = flag_off + 16 + 1024;
@@ -822,6 +832,7 @@ cache_decode_short_kernel(const __grid_constant__ CUtensorMap kmap, const __grid
   }
   sm100::mbar_fence_init();
   __syncthreads();
+  if (blocks > 1) ClusterJoin::begin();
   dam_chain_prologue();
   const int pos = __ldg(a.pos + b), cu0 = __ldg(c.cu + b), cu1 = __ldg(c.cu + b + 1);
   const typename WS::Query q = WS::fetch_q(reinterpret_cast<const T*>(a.q) + ((int64_t)b * a.Hq + h0) * D, nh);
@@ -883,22 +894,18 @@ cache_decode_short_kernel(const __grid_constant__ CUtensorMap kmap, const __grid
     stage = stage + 1 == STAGES ? 0 : stage + 1;
     ahead = ahead + 1 == STAGES ? 0 : ahead + 1;
   }
+  // (a sequence whose position lies outside its capacity has no chunk: O = 0, LSE = -inf)
   ws.store(mg + warp * (kGMaxGroup * WS::kRow));
   __syncthreads();
-  // (a sequence whose position lies outside its capacity has no chunk: O = 0, LSE = -inf)
-  float* folded = mg + kSWarps * kGMaxGroup * WS::kRow;
-  for (int e = 4 * tid; e < nh * D; e += 4 * kThreads) {
-    const int g = e / D, p = e % D;
-    Fold f;
-    f.template warps<kSWarps>(mg + g * WS::kRow, kGMaxGroup * WS::kRow, D, p);
-    if (blocks == 1) {
-      f.template write<D>(O + g * D, lse + g, p);
-    } else {
-      *reinterpret_cast<float4*>(folded + g * WS::kRow + p) = f.o;
-      if (p == 0) { folded[g * WS::kRow + D] = f.m; folded[g * WS::kRow + D + 1] = f.l; }
+  if (blocks > 1) {
+    ClusterJoin(sm + LY::join_off).template join<D, kSWarps>(mg, WS::kRow, nh, O, lse);
+  } else {
+    for (int e = 4 * tid; e < nh * D; e += 4 * kThreads) {
+      Fold f;
+      f.template warps<kSWarps>(mg + e / D * WS::kRow, kGMaxGroup * WS::kRow, D, e % D);
+      f.template write<D>(O + e / D * D, lse + e / D, e % D);
     }
   }
-  if (blocks > 1) fold_cluster<D, kSMaxSplit>(folded, WS::kRow, nh, kThreads, O, lse);
   sm100::report_expired_wait(gave_up, a.scratch + 1, (uint32_t)DAM_ERR_DEVICE_TIMEOUT);
 }
 
@@ -909,7 +916,6 @@ constexpr int kMWarps = 5, kMStages = 2, kMBlocks = 4;
 constexpr int kScales = 2 * kSlice * 4;         // bytes of the scales of a slice
 
 constexpr int kGRoundWords = 128;     // pattern words expanded per round (at most 4096 keys)
-constexpr int kGMaxSplit = 8;         // blocks of a cluster (the largest portable size)
 
 // One round of the key list of `G` heads (h0, h0 + 1, ...): kGRoundWords pattern words from word w0 on, a thread per word, the
 // words of all heads OR-ed.  A listed key is stored as (word, bit) of the round in `codes`; which heads keep it is read back
@@ -986,20 +992,21 @@ __device__ __forceinline__ int expand_round(const unsigned char* blob, const Dam
   return total;
 }
 
-template <int D>
+template <int D, bool CLUSTER>
 struct MaskedLayout {
   static constexpr int ring = kMWarps * kMStages * (Rows<D, 1>::bytes + kScales);
-  static constexpr int merge = (kMWarps + 1) * kGMaxGroup * (D + 4) * 4;        // the merge reuses the ring
+  static constexpr int merge = kMWarps * kGMaxGroup * (D + 4) * 4;              // the merge reuses the ring
   static constexpr int codes_off = ring > merge ? ring : merge;                 // u16 per listed key: round-local word * 32 + bit
   static constexpr int words_off = codes_off + kGRoundWords * 32 * 2;           // u32 [head][round-local word]
-  static constexpr int total = words_off + kGMaxGroup * kGRoundWords * 4;
+  static constexpr int join_off = words_off + kGMaxGroup * kGRoundWords * 4;
+  static constexpr int total = join_off + (CLUSTER ? ClusterJoin::bytes : 0);
 };
 
 template <typename T, int D, int CODE, bool CLUSTER>
-__global__ void __launch_bounds__(kMWarps * 32, sizeof(T) == 4 ? 3 : kMBlocks)
+__global__ void __launch_bounds__(kMWarps * 32, CLUSTER || sizeof(T) == 4 ? 3 : kMBlocks)
 cache_decode_masked_kernel(CacheDecode a, DamCacheView c, const unsigned char* __restrict__ blob) {
   dam_chain_prologue();
-  using LY = MaskedLayout<D>;
+  using LY = MaskedLayout<D, CLUSTER>;
   using WS = WarpState<T, D, CODE>;
   constexpr int kThreads = kMWarps * 32;
   extern __shared__ __align__(128) unsigned char sm[];
@@ -1032,6 +1039,7 @@ cache_decode_masked_kernel(CacheDecode a, DamCacheView c, const unsigned char* _
     }
     return;                                                  // (all blocks of a cluster)
   }
+  if constexpr (CLUSTER) ClusterJoin::begin();
   const DamSeq sq = reinterpret_cast<const DamSeq*>(blob + H->off_seq)[b];
   const int L = sq.L, W = sq.W;
   const bool in_window = pos < L;
@@ -1096,20 +1104,14 @@ cache_decode_masked_kernel(CacheDecode a, DamCacheView c, const unsigned char* _
   float* mg = reinterpret_cast<float*>(sm);
   ws.store(mg + warp * (kGMaxGroup * WS::kRow));
   __syncthreads();
-  float* folded = mg + kMWarps * kGMaxGroup * WS::kRow;
-  for (int e = 4 * tid; e < nh * D; e += 4 * kThreads) {
-    const int g = e / D, p = e % D;
-    Fold f;
-    f.template warps<kMWarps>(mg + g * WS::kRow, kGMaxGroup * WS::kRow, D, p);
-    if constexpr (CLUSTER) {
-      *reinterpret_cast<float4*>(folded + g * WS::kRow + p) = f.o;
-      if (p == 0) { folded[g * WS::kRow + D] = f.m; folded[g * WS::kRow + D + 1] = f.l; }
-    } else {
-      f.template write<D>(O + g * D, lse + g, p);
-    }
-  }
   if constexpr (CLUSTER) {
-    fold_cluster<D, kGMaxSplit>(folded, WS::kRow, nh, kThreads, O, lse);
+    ClusterJoin(sm + LY::join_off).template join<D, kMWarps>(mg, WS::kRow, nh, O, lse);
+  } else {
+    for (int e = 4 * tid; e < nh * D; e += 4 * kThreads) {
+      Fold f;
+      f.template warps<kMWarps>(mg + e / D * WS::kRow, kGMaxGroup * WS::kRow, D, e % D);
+      f.template write<D>(O + e / D * D, lse + e / D, e % D);
+    }
   }
 }
 
@@ -1204,16 +1206,16 @@ cudaError_t launch_dense(CacheDecode a, const DamCacheView& c, const dam_cache_t
 
 template <typename T, int D, int CODE>
 cudaError_t launch_masked(const CacheDecode& a, const DamCacheView& c, const void* mask, cudaStream_t st) {
-  using LY = MaskedLayout<D>;
+  constexpr int kOne = MaskedLayout<D, false>::total, kMany = MaskedLayout<D, true>::total;
   int sms = 0;
-  cudaError_t e = opt_in<cache_decode_masked_kernel<T, D, CODE, false>, LY::total>(DAM_SETUP_CACHE_SMEM + 8 + kInstance<T, D, CODE>, &sms);
-  if (e == cudaSuccess) e = opt_in<cache_decode_masked_kernel<T, D, CODE, true>, LY::total>(DAM_SETUP_CACHE_SMEM + 16 + kInstance<T, D, CODE>, &sms);
+  cudaError_t e = opt_in<cache_decode_masked_kernel<T, D, CODE, false>, kOne>(DAM_SETUP_CACHE_SMEM + 8 + kInstance<T, D, CODE>, &sms);
+  if (e == cudaSuccess) e = opt_in<cache_decode_masked_kernel<T, D, CODE, true>, kMany>(DAM_SETUP_CACHE_SMEM + 16 + kInstance<T, D, CODE>, &sms);
   if (e != cudaSuccess) return e;
   const int64_t units = (int64_t)c.num_seqs * c.Hkv * a.NS;
   const int split = masked_split(units, sms);
   if (units * split > 0x7FFFFFFF) return cudaErrorNotSupported;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)(units * split)); cfg.blockDim = dim3(kMWarps * 32); cfg.dynamicSmemBytes = LY::total; cfg.stream = st;
+  cfg.gridDim = dim3((unsigned)(units * split)); cfg.blockDim = dim3(kMWarps * 32); cfg.dynamicSmemBytes = split > 1 ? kMany : kOne; cfg.stream = st;
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
