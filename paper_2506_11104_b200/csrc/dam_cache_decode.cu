@@ -1115,13 +1115,12 @@ cache_decode_masked_kernel(CacheDecode a, DamCacheView c, const unsigned char* _
   }
 }
 
-// Blocks per (sequence, KV head, group): as for a bf16 cache (decode_split in dam_decode_mma.cu, where it is measured).
-int masked_split(int64_t units, int sm_count) {
-  if (units * 8 <= 3 * sm_count) return 8;
-  if (units * 16 <= 15 * sm_count) return 4;
-  if (units <= 2 * sm_count) return 2;
-  return 1;
-}
+// Blocks per (sequence, KV head, group): a block spends 4 us before its first rows arrive and then streams its list, so sharing the
+// list pays as long as all clusters are resident at once: 48 of 8 blocks (three per SM), 104 of 4, 222 of 2.  us a pass with 8 / 4 /
+// 2 / 1 blocks (4 heads of one KV head, head_dim 128, 4000 tokens, window 1024):
+//    40 units   8.5 /  8.6 /  9.5 / 13.1        104 units   20.2 / 10.1 / 10.9 / 13.2        222 units   36.2 / 22.6 / 12.8 / 17.3
+//    56        13.5 /  9.6 /  9.7 / 13.1        112         21.1 / 14.4 / 11.3 / 13.2        240         37.8 / 23.5 / 17.3 / 18.4
+int masked_split(int64_t units) { return units <= 48 ? 8 : units <= 104 ? 4 : units <= 222 ? 2 : 1; }
 
 // the shared memory a kernel wants, asked for once per device (KEY: a set-up step of its own per instance)
 template <auto KERNEL, int BYTES, bool LARGE_CLUSTER = false>
@@ -1212,7 +1211,7 @@ cudaError_t launch_masked(const CacheDecode& a, const DamCacheView& c, const voi
   if (e == cudaSuccess) e = opt_in<cache_decode_masked_kernel<T, D, CODE, true>, kMany>(DAM_SETUP_CACHE_SMEM + 16 + kInstance<T, D, CODE>, &sms);
   if (e != cudaSuccess) return e;
   const int64_t units = (int64_t)c.num_seqs * c.Hkv * a.NS;
-  const int split = masked_split(units, sms);
+  const int split = masked_split(units);
   if (units * split > 0x7FFFFFFF) return cudaErrorNotSupported;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(units * split)); cfg.blockDim = dim3(kMWarps * 32); cfg.dynamicSmemBytes = split > 1 ? kMany : kOne; cfg.stream = st;
