@@ -299,7 +299,7 @@ typedef struct dam_cache_t {
   void* v_codes;
   float* k_scales;                /* DEVICE, [scale rows, Hkv]: block j of sequence b in row        */
   float* v_scales;                /*   cu[b] / block_tokens + b + j (dam_cache_sizes: how many rows) */
-  int64_t k_stride_tok, k_stride_head; /* bytes, multiples of 16, head_dim contiguous               */
+  int64_t k_stride_tok, k_stride_head; /* bytes, multiples of 16, head_dim contiguous; tokens less than 2^31 apart */
   int64_t v_stride_tok, v_stride_head;
 } dam_cache_t;
 

@@ -470,6 +470,7 @@ dam_status_t check_cache(const dam_cache_t* c, bool buffers) {
   const int64_t st[4] = {c->k_stride_tok, c->k_stride_head, c->v_stride_tok, c->v_stride_head};
   for (int i = 0; i < 4; ++i)
     if (st[i] < c->head_dim || st[i] % 16) return DAM_ERR_INVALID_ARGUMENT;
+  if (c->k_stride_tok > 0x7FFFFFFF || c->v_stride_tok > 0x7FFFFFFF) return DAM_ERR_UNSUPPORTED;
   if (buffers && (!c->k_codes || !c->v_codes || !c->k_scales || !c->v_scales || !aligned(c->k_codes, 16) || !aligned(c->v_codes, 16) ||
                   !aligned(c->k_scales, 4) || !aligned(c->v_scales, 4)))
     return DAM_ERR_INVALID_ARGUMENT;

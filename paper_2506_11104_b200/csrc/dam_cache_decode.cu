@@ -915,78 +915,90 @@ cache_decode_short_kernel(const __grid_constant__ CUtensorMap kmap, const __grid
 constexpr int kMWarps = 5, kMStages = 2, kMBlocks = 4;
 constexpr int kScales = 2 * kSlice * 4;         // bytes of the scales of a slice
 
-constexpr int kGRoundWords = 128;     // pattern words expanded per round (at most 4096 keys)
+constexpr int kRoundWords = 64;       // pattern words expanded per round (at most 2048 keys)
 
-// One round of the key list of `G` heads (h0, h0 + 1, ...): kGRoundWords pattern words from word w0 on, a thread per word, the
-// words of all heads OR-ed.  A listed key is stored as (word, bit) of the round in `codes`; which heads keep it is read back
-// from the round's words in `whs`, [head][word].  By all threads of the block (WARPS warps, at least kGRoundWords threads);
-// returns the number of listed keys.
+// A listed key: which of the group's heads keep it (bits 0 .. 7), and the column (bits 9 ...) or, with bit 8, the diagonal it is on
+// (both lie below the window, whose map of L^2 bits fits a memory: far below 2^23).
+__device__ __forceinline__ int listed_key(uint32_t entry, int pos) {
+  const int at = (int)(entry >> 9);
+  return entry & 256u ? pos - at : at;
+}
+
+// One round of the key list of `G` heads (h0, h0 + 1, ...): kRoundWords pattern words from word w0 on, a thread per word, the words
+// of all heads OR-ed into `list`.  `words`: kGMaxGroup + 2 rows of kRoundWords words.  By all threads of the block; returns the number
+// of listed keys.
 template <int WARPS>
 __device__ __forceinline__ int expand_round(const unsigned char* blob, const DamHeader* H, const DamSeq& sq, int h0, int G, bool in_window,
-                                            int pos, int w0, int nwords, unsigned short* codes, uint32_t* whs, int* warp_tot,
-                                            uint64_t keep_policy) {
+                                            int pos, int w0, int nwords, uint32_t* list, uint32_t* words, uint64_t keep_policy) {
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, W = sq.W;
-  const int wi = w0 + tid;
-  const bool mine = tid < kGRoundWords && wi < nwords;    // (threads beyond the round's words hold no word)
-  // The words of all heads are requested before any is looked at: one trip to memory, not one per head.  Below the window, word
-  // wi >= W holds diagonals: diagonal r = 32 (wi - W) + k selects key pos - r; dropped when that key is a matched column of the head
-  // (then it is in the list already): bit k of the reversed 32-bit window of V that ends at key pos - 32 (wi - W).
-  const bool diagonals = mine && !in_window && wi >= W;
-  const DamHeadBits hb = dam_head_bits(blob, H, sq, h0);
-  const uint32_t* word = in_window ? hb.M + (size_t)pos * W + wi : wi < W ? hb.V + wi : hb.D + (wi - W);
-  const int64_t per_head = in_window ? (int64_t)sq.L * W : 3ll * W;
-  const int x = pos - 32 * (wi - W) - 31, xw = x >> 5;
-  uint32_t wh[kGMaxGroup], uni = 0u;
+  const int used = min(kRoundWords, nwords - w0);
+  uint32_t* const unions = words + kGMaxGroup * kRoundWords;
+  uint32_t* const begins = unions + kRoundWords;
+  __syncthreads();                                        // the previous round's list is no longer read
+  if (warp * 32 < kRoundWords) {
+    uint32_t uni = 0u;
+    if (warp * 32 < used) {
+      const int wi = w0 + tid;
+      const bool mine = tid < used;
+      // The words of all heads are requested before any is looked at: one trip to memory, not one per head.  Below the window,
+      // word wi >= W holds diagonals: diagonal r = 32 (wi - W) + k selects key pos - r; dropped when that key is a matched column
+      // of the head (then it is in the list already): bit k of the reversed 32-bit window of V that ends at key pos - 32 (wi - W).
+      const bool diagonals = mine && !in_window && wi >= W;
+      const int own = pos - 32 * wi;                      // bit of the word that is the row's own position
+      const uint32_t upto = own < 0 ? 0u : own >= 31 ? 0xFFFFFFFFu : (2u << own) - 1u;
+      const DamHeadBits hb = dam_head_bits(blob, H, sq, h0);
+      const uint32_t* word = in_window ? hb.M + (size_t)pos * W + wi : wi < W ? hb.V + wi : hb.D + (wi - W);
+      const int64_t per_head = in_window ? (int64_t)sq.L * W : 3ll * W;
+      const int x = pos - 32 * (wi - W) - 31, xw = x >> 5;
 #pragma unroll
-  for (int g0 = 0; g0 < kGMaxGroup; g0 += 4) {            // (four heads at a time: most groups have no more)
-    uint32_t lo[4], hi[4];
+      for (int g0 = 0; g0 < kGMaxGroup; g0 += 4) {        // (four heads at a time: most groups have no more)
+        uint32_t wh[4], lo[4], hi[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int g = g0 + i;
-      wh[g] = lo[i] = hi[i] = 0u;
-      if (g0 < G) {
-        if (mine && g < G) wh[g] = ldg_keep(word + g * per_head, keep_policy);
-        if (diagonals && g < G && xw >= 0 && xw < W) lo[i] = ldg_keep(hb.V + 3ll * W * g + xw, keep_policy);
-        if (diagonals && g < G && xw + 1 >= 0 && xw + 1 < W) hi[i] = ldg_keep(hb.V + 3ll * W * g + xw + 1, keep_policy);
+        for (int i = 0; i < 4; ++i) {
+          const int g = g0 + i;
+          wh[i] = lo[i] = hi[i] = 0u;
+          if (g0 < G) {
+            if (mine && g < G) wh[i] = ldg_keep(word + g * per_head, keep_policy);
+            if (diagonals && g < G && xw >= 0 && xw < W) lo[i] = ldg_keep(hb.V + 3ll * W * g + xw, keep_policy);
+            if (diagonals && g < G && xw + 1 >= 0 && xw + 1 < W) hi[i] = ldg_keep(hb.V + 3ll * W * g + xw + 1, keep_policy);
+          }
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          wh[i] &= ~__brev(__funnelshift_r(lo[i], hi[i], x & 31));
+          if (in_window) wh[i] &= upto;                   // (a map of the caller's may have cells above its diagonal)
+          words[(g0 + i) * kRoundWords + tid] = wh[i];
+          uni |= wh[i];
+        }
       }
     }
+    // where the keys of a word begin in the list: within the warp's words (the other warp's are added below)
+    const int cnt = __popc(uni);
+    int off = cnt;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      wh[g0 + i] &= ~__brev(__funnelshift_r(lo[i], hi[i], x & 31));
-      uni |= wh[g0 + i];
+    for (int o = 1; o < 32; o <<= 1) {
+      const int y = __shfl_up_sync(0xFFFFFFFFu, off, o);
+      if (lane >= o) off += y;
     }
-  }
-  const int cnt = __popc(uni);
-  int off = cnt;
-#pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
-    const int y = __shfl_up_sync(0xFFFFFFFFu, off, o);
-    if (lane >= o) off += y;
-  }
-  __syncthreads();                                        // the previous round's list is no longer read
-  if (lane == 31) warp_tot[warp] = off;
-  if (tid < kGRoundWords) {
-#pragma unroll
-    for (int g = 0; g < kGMaxGroup; ++g) whs[g * kGRoundWords + tid] = wh[g];
+    unions[tid] = uni;
+    begins[tid] = (uint32_t)(off - cnt);
   }
   __syncthreads();
-  int total = 0, before = 0;
-#pragma unroll
-  for (int w = 0; w < WARPS; ++w) {
-    const int wt = warp_tot[w];
-    if (w < warp) before += wt;
-    total += wt;
-  }
+  static_assert(kRoundWords == 64, "two warps have the words");
+  const int first = (int)begins[31] + __popc(unions[31]), total = first + (int)begins[63] + __popc(unions[63]);
   // the words are spread to the warps, a lane per bit (a thread that took its own word's bits one by one needed up to 32 steps, and
   // the words of a band are full)
-  __shared__ uint2 listed[kGRoundWords];
-  if (tid < kGRoundWords) listed[tid] = make_uint2(uni, (uint32_t)(off + before - cnt));
-  __syncthreads();
-  const int used = min(kGRoundWords, nwords - w0);
-#pragma unroll 4
   for (int w = warp; w < used; w += WARPS) {
-    const uint2 l = listed[w];
-    if (l.x >> lane & 1u) codes[l.y + __popc(l.x & ((1u << lane) - 1u))] = (unsigned short)(w * 32 + lane);
+    const uint32_t uni = unions[w];
+    if (uni >> lane & 1u) {
+      uint32_t heads = 0u;
+#pragma unroll
+      for (int g = 0; g < kGMaxGroup; ++g)
+        if (g < 4 || G > 4) heads |= (words[g * kRoundWords + w] >> lane & 1u) << g;
+      const int wi = w0 + w;
+      const uint32_t at = in_window || wi < W ? 32u * wi + lane : 32u * (wi - W) + lane;
+      list[begins[w] + (w < 32 ? 0 : first) + __popc(uni & ((1u << lane) - 1u))] = at << 9 | (in_window || wi < W ? 0u : 256u) | heads;
+    }
   }
   __syncthreads();
   return total;
@@ -996,9 +1008,9 @@ template <int D, bool CLUSTER>
 struct MaskedLayout {
   static constexpr int ring = kMWarps * kMStages * (Rows<D, 1>::bytes + kScales);
   static constexpr int merge = kMWarps * kGMaxGroup * (D + 4) * 4;              // the merge reuses the ring
-  static constexpr int codes_off = ring > merge ? ring : merge;                 // u16 per listed key: round-local word * 32 + bit
-  static constexpr int words_off = codes_off + kGRoundWords * 32 * 2;           // u32 [head][round-local word]
-  static constexpr int join_off = words_off + kGMaxGroup * kGRoundWords * 4;
+  static constexpr int list_off = ring > merge ? ring : merge;
+  static constexpr int words_off = list_off + kRoundWords * 32 * 4;
+  static constexpr int join_off = words_off + (kGMaxGroup + 2) * kRoundWords * 4;
   static constexpr int total = join_off + (CLUSTER ? ClusterJoin::bytes : 0);
 };
 
@@ -1010,9 +1022,8 @@ cache_decode_masked_kernel(CacheDecode a, DamCacheView c, const unsigned char* _
   using WS = WarpState<T, D, CODE>;
   constexpr int kThreads = kMWarps * 32;
   extern __shared__ __align__(128) unsigned char sm[];
-  __shared__ int warp_tot[kMWarps];
-  unsigned short* codes = reinterpret_cast<unsigned short*>(sm + LY::codes_off);
-  uint32_t* whs = reinterpret_cast<uint32_t*>(sm + LY::words_off);
+  uint32_t* list = reinterpret_cast<uint32_t*>(sm + LY::list_off);
+  uint32_t* words = reinterpret_cast<uint32_t*>(sm + LY::words_off);
   const int nsplit = CLUSTER ? (int)cooperative_groups::this_cluster().num_blocks() : 1;
   const int split = CLUSTER ? (int)cooperative_groups::this_cluster().block_rank() : 0;
   const int heads = c.Hkv * a.NS, unit = blockIdx.x / nsplit, hg = unit % heads, b = unit / heads;
@@ -1052,25 +1063,25 @@ cache_decode_masked_kernel(CacheDecode a, DamCacheView c, const unsigned char* _
   ws.set_q(q, nh, a.scale_log2);
   const uint32_t ring = static_cast<uint32_t>(__cvta_generic_to_shared(sm)) + warp * (kMStages * (Rows<D, 1>::bytes + kScales));
   const uint64_t stream_policy = l2_evict_first_policy(), keep_policy = l2_evict_last_policy();
-  for (int w0 = 0; w0 < nwords; w0 += kGRoundWords) {
-    const int total = expand_round<kMWarps>(blob, H, sq, h0, nh, in_window, pos, w0, nwords, codes, whs, warp_tot, keep_policy);
-    auto key_of = [&](uint32_t code) -> int {
-      const int w = w0 + (int)(code >> 5), k = (int)(code & 31u);
-      return (in_window || w < W) ? 32 * w + k : pos - (32 * (w - W) + k);
-    };
+  constexpr int P = Rows<D, 1>::pieces, kRowsAtOnce = 32 / P;
+  const unsigned char *kp = Kb + lane % P * 16, *vp = Vb + lane % P * 16;
+  const float* sp = (lane < 16 ? c.ks : c.vs) + row0 * c.Hkv + kvh;
+  const int kst = (int)c.kst, vst = (int)c.vst;              // (the host has seen to it that they are 32-bit numbers)
+  for (int w0 = 0; w0 < nwords; w0 += kRoundWords) {
+    const int total = expand_round<kMWarps>(blob, H, sq, h0, nh, in_window, pos, w0, nwords, list, words, keep_policy);
     const int nslices = (total + kSlice - 1) / kSlice, first = split * kMWarps + warp, step = nsplit * kMWarps;
     auto issue = [&](int s, int stage) {
       const uint32_t dst = ring + stage * (Rows<D, 1>::bytes + kScales);
+      // lane: key `lane & 15` of the slice (places past the end repeat the first key; nobody keeps them below)
+      const int idx = s * kSlice + (lane & 15), j = listed_key(list[idx < total ? idx : s * kSlice], pos);
 #pragma unroll
-      for (int i = 0; i < kSlice * Rows<D, 1>::pieces / 32; ++i) {
-        const int x = lane + 32 * i, r = x / Rows<D, 1>::pieces, piece = x % Rows<D, 1>::pieces, idx = s * kSlice + r;
-        const int j = key_of(codes[idx < total ? idx : s * kSlice]);    // places past the end repeat the slice's first key (not kept below)
-        const uint32_t at = Rows<D, 1>::at(r, piece);
-        cp_async16(dst + at, Kb + (int64_t)j * c.kst + piece * 16, stream_policy);
-        cp_async16(dst + Rows<D, 1>::v_off + at, Vb + (int64_t)j * c.vst + piece * 16, stream_policy);
+      for (int i = 0; i < kSlice / kRowsAtOnce; ++i) {
+        const int r = lane / P + kRowsAtOnce * i, key = __shfl_sync(0xFFFFFFFFu, j, r);
+        const uint32_t at = Rows<D, 1>::at(r, lane % P);
+        cp_async16(dst + at, kp + (int64_t)key * kst, stream_policy);
+        cp_async16(dst + Rows<D, 1>::v_off + at, vp + (int64_t)key * vst, stream_policy);
       }
-      const int idx = s * kSlice + (lane & 15), j = key_of(codes[idx < total ? idx : s * kSlice]);
-      cp_async4_zfill(dst + Rows<D, 1>::bytes + 4 * lane, (lane < 16 ? c.ks : c.vs) + (row0 + (j >> c.shift)) * c.Hkv + kvh, 4u);
+      cp_async4_zfill(dst + Rows<D, 1>::bytes + 4 * lane, sp + (int64_t)(j >> c.shift) * c.Hkv, 4u);
     };
 #pragma unroll
     for (int s = 0; s < kMStages - 1; ++s) {
@@ -1087,11 +1098,7 @@ cache_decode_masked_kernel(CacheDecode a, DamCacheView c, const unsigned char* _
 #pragma unroll
       for (int k = 0; k < 2; ++k) {
         const int idx = s * kSlice + Rows<D, 1>::key(row) + 8 * k;
-        if (idx < total) {
-          const uint32_t code = codes[idx];
-#pragma unroll
-          for (int e = 0; e < 2; ++e) keep |= (whs[(2 * quad + e) * kGRoundWords + (code >> 5)] >> (code & 31u) & 1u) << (2 * k + e);
-        }
+        if (idx < total) keep |= (list[idx] >> (2 * quad) & 3u) << (2 * k);
       }
       const uint32_t slice = ring + it % kMStages * (Rows<D, 1>::bytes + kScales);
       ws.template step<WS::kKeep, 1>(slice, slice + Rows<D, 1>::bytes, keep);
