@@ -795,28 +795,31 @@ cache_join_kernel(CacheDecode a, DamCacheView c, const float* __restrict__ parti
 // ---- every key of short sequences ---------------------------------------------------------------
 // One block, or a cluster of up to sixteen, per (sequence, KV head, group of 8 heads): a single launch, and nothing to look up before
 // the first copy but the sequence's own position and bounds.  The partial results of a cluster's blocks meet in shared memory.
-constexpr int kSWarps = 8;
-
-template <int D>
+// kAlone: blocks of eight warps, one per SM.  kPairs, kFours: two of eight or four of four warps per SM, whose beginnings and ends fall
+// under one another's work; no clusters.
+enum ShortForm { kAlone, kPairs, kFours };
+template <int D, ShortForm FORM>
 struct ShortLayout {
-  static constexpr int stages = D == 128 ? 2 : 4;
-  static constexpr int ring = kSWarps * stages * Rows<D, kTile>::bytes;
-  static constexpr int merge_off = ring, merge = kSWarps * kGMaxGroup * (D + 4) * 4;
-  static constexpr int join_off = merge_off + merge, scale_off = join_off + ClusterJoin::bytes;
-  static constexpr int bar_off = scale_off + kSWarps * stages * kTile * 8;
-  static constexpr int flag_off = bar_off + kSWarps * stages * 8;
+  static constexpr int warps = FORM == kFours ? 4 : 8, blocks = FORM == kAlone ? 1 : FORM == kPairs ? 2 : 4;   // blocks per SM
+  static constexpr int stages = (FORM == kAlone ? 2 : 1) * (D == 128 ? 1 : 2);
+  static constexpr int ring = warps * stages * Rows<D, kTile>::bytes;
+  static constexpr int merge_off = ring, merge = warps * kGMaxGroup * (D + 4) * 4;
+  static constexpr int join_off = merge_off + merge, scale_off = join_off + (FORM == kAlone ? ClusterJoin::bytes : 0);
+  static constexpr int bar_off = scale_off + warps * stages * kTile * 8;
+  static constexpr int flag_off = bar_off + warps * stages * 8;
   static constexpr int total = flag_off + 16 + 1024;
 };
 
-template <typename T, int D, int CODE>
-__global__ void __launch_bounds__(kSWarps * 32, 1)
+template <typename T, int D, int CODE, ShortForm FORM>
+__global__ void __launch_bounds__(ShortLayout<D, FORM>::warps * 32, (ShortLayout<D, FORM>::blocks))
 cache_decode_short_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUtensorMap vmap, CacheDecode a, DamCacheView c) {
-  using LY = ShortLayout<D>;
+  using LY = ShortLayout<D, FORM>;
   using WS = WarpState<T, D, CODE>;
-  constexpr int STAGES = LY::stages, kThreads = kSWarps * 32, kChunk = kSWarps * kKeys;
+  constexpr int WARPS = LY::warps, STAGES = LY::stages, kThreads = WARPS * 32, kChunk = WARPS * kKeys;
   extern __shared__ unsigned char sm_raw[];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  const int blocks = (int)cooperative_groups::this_cluster().num_blocks(), rank = (int)cooperative_groups::this_cluster().block_rank();
+  const int blocks = FORM != kAlone ? 1 : (int)cooperative_groups::this_cluster().num_blocks();
+  const int rank = FORM != kAlone ? 0 : (int)cooperative_groups::this_cluster().block_rank();
   const int heads = c.Hkv * a.NS, unit = blockIdx.x / blocks, b = unit / heads, hg = unit - b * heads;
   const int kvh = hg / a.NS, sub = hg - kvh * a.NS, h0 = kvh * a.G + sub * kGMaxGroup, nh = min(kGMaxGroup, a.G - sub * kGMaxGroup);
   unsigned char* sm = sm_raw + (-sm100::smem_u32(sm_raw) & 1023u);
@@ -882,6 +885,7 @@ cache_decode_short_kernel(const __grid_constant__ CUtensorMap kmap, const __grid
     cp_async_commit();
     cp_async_wait<STAGES - 1>();
     __syncwarp();
+    // (with one stage the copy has just been asked for, and the other warps of the SM cover the wait)
     const int live = len - (key0 + it * kChunk);
     if (live > 0 && !lost) {
       lost = !sm100::mbar_wait(bars + 8 * stage, phases >> stage & 1u, gave_up);
@@ -898,11 +902,11 @@ cache_decode_short_kernel(const __grid_constant__ CUtensorMap kmap, const __grid
   ws.store(mg + warp * (kGMaxGroup * WS::kRow));
   __syncthreads();
   if (blocks > 1) {
-    ClusterJoin(sm + LY::join_off).template join<D, kSWarps>(mg, WS::kRow, nh, O, lse);
+    ClusterJoin(sm + LY::join_off).template join<D, WARPS>(mg, WS::kRow, nh, O, lse);
   } else {
     for (int e = 4 * tid; e < nh * D; e += 4 * kThreads) {
       Fold f;
-      f.template warps<kSWarps>(mg + e / D * WS::kRow, kGMaxGroup * WS::kRow, D, e % D);
+      f.template warps<WARPS>(mg + e / D * WS::kRow, kGMaxGroup * WS::kRow, D, e % D);
       f.template write<D>(O + e / D * D, lse + e / D, e % D);
     }
   }
@@ -1157,6 +1161,32 @@ int short_split(int64_t units, int64_t longest, int chunk) {
 }
 // capacity per block up to which they are short: large clusters leave more SMs without one
 int64_t short_keys(int split) { return split >= 8 ? 1024 : 2048; }
+// Batches of more (sequence, KV head, group) than SMs, in us a pass (capacities of equal length; 8 KV heads of 128, int8 / 4 of 64, fp32
+// queries; one block each as kPairs, as kFours, or the list that all SMs share):
+//    20 x 1000   13 / 20 / 16        64 x 1000   26 / 25 / 39        256 x 500   54 / 46 / 113        64 x 8000   145 / 152 / 135
+//    40 x 3000   45 / 54 / 46        64 x 4000   76 / 80 / 80        64 x 1000 of 64  9 / 13 / 18     64 x 4000 of 64  25 / 41 / 32
+// A block each, then, up to 4096 tokens, unless one sequence is longer than an SM's part of all of them.
+constexpr int64_t kManyKeys = 4096;
+
+template <typename T, int D, int CODE, ShortForm FORM>
+cudaError_t launch_short(const CacheDecode& a, const DamCacheView& c, const CUtensorMap& kmap, const CUtensorMap& vmap, int64_t units, int split,
+                         cudaStream_t st) {
+  using LY = ShortLayout<D, FORM>;
+  if (units * split > 0x7FFFFFFF) return cudaErrorNotSupported;
+  int sms = 0;
+  const cudaError_t e = opt_in<cache_decode_short_kernel<T, D, CODE, FORM>, LY::total, FORM == kAlone>(
+      DAM_SETUP_CACHE_SMEM + 24 + 8 * FORM + kInstance<T, D, CODE>, &sms);
+  if (e != cudaSuccess) return e;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)(units * split)); cfg.blockDim = dim3(LY::warps * 32); cfg.dynamicSmemBytes = LY::total; cfg.stream = st;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = (unsigned)split; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr; cfg.numAttrs = FORM == kAlone ? 2 : 1;
+  return cudaLaunchKernelEx(&cfg, cache_decode_short_kernel<T, D, CODE, FORM>, kmap, vmap, a, c);
+}
 
 template <typename T, int D, int CODE>
 cudaError_t launch_dense(CacheDecode a, const DamCacheView& c, const dam_cache_t* cache, cudaStream_t st) {
@@ -1180,20 +1210,11 @@ cudaError_t launch_dense(CacheDecode a, const DamCacheView& c, const dam_cache_t
   const int blocks = sms < kMaxShares ? sms : kMaxShares;
 
   const int64_t units = heads * c.num_seqs;
-  const int split = short_split(units, longest, kSWarps * kKeys);
-  if (split && longest <= split * short_keys(split)) {
-    e = opt_in<cache_decode_short_kernel<T, D, CODE>, ShortLayout<D>::total, true>(DAM_SETUP_CACHE_SMEM + 24 + kInstance<T, D, CODE>, &sms);
-    if (e != cudaSuccess) return e;
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(units * split)); cfg.blockDim = dim3(kSWarps * 32); cfg.dynamicSmemBytes = ShortLayout<D>::total; cfg.stream = st;
-    cudaLaunchAttribute attr[2];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    attr[1].id = cudaLaunchAttributeClusterDimension;
-    attr[1].val.clusterDim.x = (unsigned)split; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
-    cfg.attrs = attr; cfg.numAttrs = 2;
-    return cudaLaunchKernelEx(&cfg, cache_decode_short_kernel<T, D, CODE>, kmap, vmap, a, c);
-  }
+  const int split = short_split(units, longest, ShortLayout<D, kAlone>::warps * kKeys);
+  if (split && longest <= split * short_keys(split)) return launch_short<T, D, CODE, kAlone>(a, c, kmap, vmap, units, split, st);
+  if (!split && longest <= kManyKeys && longest * blocks <= cache->total_tokens * heads)
+    return units <= 4 * blocks ? launch_short<T, D, CODE, kPairs>(a, c, kmap, vmap, units, 1, st)
+                               : launch_short<T, D, CODE, kFours>(a, c, kmap, vmap, units, 1, st);
 
   // all heads side by side where that leaves no more than an eighth of the SMs without work; and no more shares than there can be
   // chunks

@@ -244,6 +244,58 @@ def test_attention_over_every_key(lengths, Hq, Hkv, d, dtype, code, block):
         _check(p, q, positions, O, lse)
 
 
+# each way of sharing the keys: a cluster per sequence, a block each (two sizes), the list with the KV heads side by side and one after
+# the other; on 148 SMs
+SHARED = [([20000, 700, 1], 4, 2, 64, BF16, "int8", 64), ([18000], 8, 1, 128, BF16, "e4m3", 128), ([9000, 17000, 3], 8, 2, 128, F32, "int8", 16),
+          ([17, 300, 64, 1, 129, 500, 33] * 29, 2, 1, 64, BF16, "e4m3", 16), ([40, 250, 129, 64, 1] * 40, 16, 4, 128, BF16, "int8", 32),
+          ([33, 128, 190] * 100, 6, 3, 64, F32, "e4m3", 64), ([17000, 100], 25, 25, 64, BF16, "int8", 64),
+          ([5000] + [1 + 3 * k for k in range(160)], 1, 1, 128, BF16, "e4m3", 64)]
+
+
+@pytest.mark.parametrize("lengths,Hq,Hkv,d,dtype,code,block", SHARED)
+def test_attention_however_the_keys_are_shared(lengths, Hq, Hkv, d, dtype, code, block):
+    rng = np.random.default_rng(22)
+    p = _filled(rng, lengths, Hkv, d, code, block, dtype)
+    q = torch.from_numpy(rng.standard_normal((len(lengths), Hq, d))).float().to(dtype).to(DEV)
+    for positions in ([n - 1 for n in lengths], [n * 2 // 3 for n in lengths]):
+        O, lse, scratch = B.dam_cache_decode_attention(q, p.cache, _ints(positions))
+        assert B.dam_poll_status(scratch) == 0
+        _check(p, q, positions, O, lse, heads=sorted({0, Hq // 2, Hq - 1}))
+    # a position outside its capacity, in the same form
+    positions[-1] = lengths[-1]
+    O2, lse2, scratch = B.dam_cache_decode_attention(q, p.cache, _ints(positions))
+    assert B.dam_poll_status(scratch) == 1
+    assert not O2[-1].any() and torch.isneginf(lse2[-1]).all()
+    # (the others' keys may be shared out differently: equal to rounding)
+    if len(lengths) > 1:
+        _check(p, q, positions[:-1], O2, lse2, heads=[Hq - 1])
+
+
+def test_attention_over_codes_by_head_and_wide_strides():
+    """Head-major codes and codes inside a wider buffer, in every form of the attention."""
+    rng = np.random.default_rng(24)
+    for lengths, d in (([500, 70], 64), ([500, 70], 128), ([18000], 128), ([60] * 200, 64)):
+        T, Hkv, Hq = sum(lengths), 1 if len(lengths) == 200 else 2, 4
+        wide = [torch.randint(-127, 128, (T, Hkv + 1, d + 16), dtype=torch.int8, device=DEV) for _ in range(2)]
+        major = [torch.randint(-127, 128, (Hkv, T, d), dtype=torch.int8, device=DEV) for _ in range(2)]
+        rows = T // 32 + len(lengths)
+        scales = [0.01 + 0.02 * torch.rand(rows, Hkv, device=DEV) for _ in range(2)]
+        q = torch.from_numpy(rng.standard_normal((len(lengths), Hq, d))).float().to(BF16).to(DEV)
+        positions = [n - 1 for n in lengths]
+        for codes in ([x[:, 1:, 16:] for x in wide], [x.permute(1, 0, 2) for x in major], [major[0].permute(1, 0, 2), wide[1][:, :Hkv, :d]]):
+            p = Pair.__new__(Pair)
+            p.Hkv, p.d, p.dtype = Hkv, d, BF16
+            p.cache = B.make_cache(_cu(lengths), Hkv, d, "int8", 32, DEV, codes[0], codes[1], scales[0], scales[1])
+            p.k, p.v = R.unpack(p.cache, "k"), R.unpack(p.cache, "v")
+            O, lse, scratch = B.dam_cache_decode_attention(q, p.cache, _ints(positions))
+            assert B.dam_poll_status(scratch) == 0
+            _check(p, q, positions, O, lse, heads=[0, Hq - 1])
+            blob, keep = _blob(rng, lengths, Hq, 64)
+            O, lse, scratch = B.dam_cache_decode_attention(q, p.cache, _ints(positions), blob)
+            assert B.dam_poll_status(scratch) == 0
+            _check(p, q, positions, O, lse, keep, heads=[0, Hq - 1])
+
+
 def test_attention_of_many_ragged_sequences():
     """More sequences than a warp has lanes, more shares than chunks and more chunks than shares."""
     rng = np.random.default_rng(23)
