@@ -582,6 +582,13 @@ struct Shares {
   }
 };
 
+// The end of a warp that has given up on a copy: those on their way (none otherwise) land before it leaves.
+__device__ __forceinline__ void drain(uint32_t bars, int stages, uint32_t phases, uint32_t pending, volatile uint32_t* gave_up) {
+  if (pending == 0u) return;
+  for (int s = 0; s < stages; ++s)
+    if (pending >> s & 1u) sm100::mbar_wait(bars + 8 * s, phases >> s & 1u, gave_up, sm100::kDrainPolls);
+}
+
 template <typename T, int D, int CODE, int WARPS, int STAGES>
 __global__ void __launch_bounds__(WARPS * 32, 1)
 cache_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUtensorMap vmap, CacheDecode a, DamCacheView c,
@@ -634,8 +641,10 @@ cache_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_const
     token = cu + key;
     sp = (lane & 1 ? c.vs : c.ks) + (int64_t)((cu >> c.shift) + in.b) * c.Hkv + kvh;
   };
+  uint32_t phases = 0u, pending = 0u;  // bit s: parity of the next copy into stage s; whether one is on its way
   auto issue = [&](int stage) {
     if (in.live <= 0) return;
+    pending |= 1u << stage;
     // (16 keys from a multiple of 16 on lie in one block.  A tile may reach into the rows behind the last key, of this sequence
     // or of the next; rows beyond the cache read as zeros.  The scale of a slice without a key is the first slice's)
     if (lane < 2 * kTile) {
@@ -671,13 +680,12 @@ cache_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_const
   WS ws;
   int stage = 0, ahead = STAGES - 1, segment = 0, since = 0;  // `since`: chunks of the present (KV head, group) behind it
   int h0 = 0, nh = 0;
-  uint32_t phases = 0u;                // bit s: parity of the next copy into stage s
-  bool lost = false;                   // a copy did not arrive
+  bool lost = false;                   // a copy did not arrive: no more are asked for
 #pragma unroll 1
   for (int it = 0; it < todo; ++it) {
     if (it + STAGES - 1 < todo) {
       advance();
-      issue(ahead);
+      if (!lost) issue(ahead);
     }
     cp_async_commit();
     if (since == 0) {
@@ -689,9 +697,10 @@ cache_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_const
     }
     cp_async_wait<STAGES - 1>();
     __syncwarp();
+    if (cur.live > 0 && !lost) lost = !sm100::mbar_wait(bars + 8 * stage, phases >> stage & 1u, gave_up);
     if (cur.live > 0 && !lost) {
-      lost = !sm100::mbar_wait(bars + 8 * stage, phases >> stage & 1u, gave_up);
       phases ^= 1u << stage;
+      pending ^= 1u << stage;
       const uint32_t rows = ring + stage * Rows<D, kTile>::bytes, sc = scales + 8 * kTile * stage;
       if (cur.live >= kKeys) ws.template step<WS::kAll, kTile>(rows, sc, 0u);
       else ws.template step<WS::kFirst, kTile>(rows, sc, (uint32_t)cur.live);
@@ -724,6 +733,7 @@ cache_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_const
     }
     if (it + 1 < todo) cur.next(c, a.pos, LY::chunk, heads);
   }
+  drain(bars, STAGES, phases, pending, gave_up);
   sm100::report_expired_wait(gave_up, a.scratch + 1, (uint32_t)DAM_ERR_DEVICE_TIMEOUT);
 }
 
@@ -847,9 +857,11 @@ cache_decode_short_kernel(const __grid_constant__ CUtensorMap kmap, const __grid
   const Shares sh(n, blocks);
   const int todo = sh.begin(rank + 1) - sh.begin(rank), key0 = sh.begin(rank) * kChunk + warp * kKeys, len = pos + 1;
   const float* sp = (lane & 1 ? c.vs : c.ks) + (int64_t)((cu0 >> c.shift) + b) * c.Hkv + kvh;
+  uint32_t phases = 0u, pending = 0u;  // bit s: parity of the next copy into stage s; whether one is on its way
   auto issue = [&](int it, int stage) {
     const int key = key0 + it * kChunk;
     if (key >= len) return;
+    pending |= 1u << stage;
     if (lane < 2 * kTile) {
       const int at = key + (key + (lane >> 1) * kSlice < len ? (lane >> 1) * kSlice : 0);
       cp_async4_zfill(scales + 8 * kTile * stage + 4 * lane, sp + (int64_t)(at >> c.shift) * c.Hkv, 4u);
@@ -877,19 +889,19 @@ cache_decode_short_kernel(const __grid_constant__ CUtensorMap kmap, const __grid
   ws.reset();
   ws.set_q(q, nh, a.scale_log2);
   int stage = 0, ahead = STAGES - 1;
-  uint32_t phases = 0u;
-  bool lost = false;
+  bool lost = false;                   // a copy did not arrive: no more are asked for
 #pragma unroll 1
   for (int it = 0; it < todo; ++it) {
-    if (it + STAGES - 1 < todo) issue(it + STAGES - 1, ahead);
+    if (it + STAGES - 1 < todo && !lost) issue(it + STAGES - 1, ahead);
     cp_async_commit();
     cp_async_wait<STAGES - 1>();
     __syncwarp();
     // (with one stage the copy has just been asked for, and the other warps of the SM cover the wait)
     const int live = len - (key0 + it * kChunk);
+    if (live > 0 && !lost) lost = !sm100::mbar_wait(bars + 8 * stage, phases >> stage & 1u, gave_up);
     if (live > 0 && !lost) {
-      lost = !sm100::mbar_wait(bars + 8 * stage, phases >> stage & 1u, gave_up);
       phases ^= 1u << stage;
+      pending ^= 1u << stage;
       const uint32_t rows = ring + stage * Rows<D, kTile>::bytes, sc = scales + 8 * kTile * stage;
       if (live >= kKeys) ws.template step<WS::kAll, kTile>(rows, sc, 0u);
       else ws.template step<WS::kFirst, kTile>(rows, sc, (uint32_t)live);
@@ -910,6 +922,7 @@ cache_decode_short_kernel(const __grid_constant__ CUtensorMap kmap, const __grid
       f.template write<D>(O + e / D * D, lse + e / D, e % D);
     }
   }
+  drain(bars, STAGES, phases, pending, gave_up);
   sm100::report_expired_wait(gave_up, a.scratch + 1, (uint32_t)DAM_ERR_DEVICE_TIMEOUT);
 }
 

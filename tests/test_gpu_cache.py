@@ -226,7 +226,7 @@ def _check(p, q, positions, O, lse, keep=None, scale=None, heads=None):
     return worst
 
 
-DECODE = [([300, 1, 129, 77], 8, 2, 128, BF16, "int8", 64), ([300, 1, 129, 77], 8, 2, 128, BF16, "e4m3", 16),
+DECODE = [([1], 4, 1, 64, BF16, "int8", 16), ([1], 8, 8, 128, F32, "e4m3", 128), ([300, 1, 129, 77], 8, 2, 128, BF16, "int8", 64), ([300, 1, 129, 77], 8, 2, 128, BF16, "e4m3", 16),
           ([2000, 500], 4, 1, 64, BF16, "int8", 32), ([1, 2, 15, 16, 17, 127, 128, 129], 8, 8, 64, BF16, "e4m3", 128),
           ([900], 16, 1, 128, BF16, "int8", 64), ([513, 1025], 12, 1, 64, BF16, "e4m3", 64), ([777], 24, 8, 128, BF16, "int8", 128),
           ([640, 333], 8, 2, 128, F32, "int8", 64), ([1500], 6, 2, 64, F32, "e4m3", 16), ([400, 3], 9, 1, 128, F32, "e4m3", 32),
