@@ -12,8 +12,8 @@
 
 namespace {
 
-constexpr int kCThreads = 256;
-constexpr int kReadShift = 6, kReadTokens = 1 << kReadShift;   // packed tokens of a read's slot
+constexpr int kRThreads = 256, kRPasses = 4, kRBlocks = 4;   // of a read: threads, 8-element pieces per thread, blocks per SM
+constexpr int kRPieces = kRThreads * kRPasses;
 
 // 8 consecutive elements as they are in memory, and as fp32
 template <typename T> struct Eight;
@@ -302,91 +302,103 @@ cache_write_one_kernel(CacheRows src, const int32_t* __restrict__ starts, DamCac
   if (lane == 0) *scale = s;
 }
 
-// Slot of a read: kReadTokens packed tokens of a sequence.  The pointers are a thread's own, as in WriteSlot.
-template <typename T, int D>
-struct ReadSlot {
-  int b, t0, cap0, start, all;   // sequence; its packed and its cache row; its tokens start .. start + all - 1
-  int zero;                      // slot `x` begins with token kReadTokens * (x - zero) of these
-  bool fits;
-  T* x;
-  const unsigned char* codes;
-  const float* scales;           // of block 0 of the sequence
-  int64_t xst, cst;
-  int64_t dx, dc;                // to the next slot of the same sequence
-  int row, p, n, readable;       // packed row and place of the slot's first token; tokens from it on; of those, how many can be read (n or none)
-  __device__ __forceinline__ uint32_t enter(const DamCacheView& c, const CacheRows& dst, const int32_t* starts, uint32_t slot) {
-    b = cache_seq_of_slot(dst.cu, c.num_seqs, kReadShift, 1, slot);
-    t0 = __ldg(dst.cu + b);
-    cap0 = __ldg(c.cu + b);
-    const int t1 = __ldg(dst.cu + b + 1);
-    all = t1 - t0;
-    fits = range_fits(c, starts, b, all, &start);
-    zero = (t0 >> kReadShift) + b;
-    return (uint32_t)(t1 >> kReadShift) + (uint32_t)(b + 1);
-  }
-  __device__ __forceinline__ bool place(const DamCacheView& c, uint32_t slot) {
-    const int64_t base = (int64_t)((int)slot - zero) << kReadShift;
-    if (base >= all) return false;
-    n = all - (int)base;
-    readable = fits ? n : 0;
-    p = fits ? start + (int)base : 0;
-    row = t0 + (int)base;
-    return true;
-  }
-  __device__ __forceinline__ void aim(const DamCacheView& c, const CacheRows& dst, int kv, int h, uint32_t step) {
-    constexpr int TPR = D / 8;
-    const int r0 = threadIdx.x / TPR, e = threadIdx.x % TPR * 8;
-    xst = kv ? dst.vst : dst.kst; cst = kv ? c.vst : c.kst;
-    const int64_t tokens = (int64_t)step << kReadShift;
-    dx = tokens * xst; dc = tokens * cst;
-    x = reinterpret_cast<T*>(const_cast<void*>(kv ? dst.V : dst.K)) + ((int64_t)row + r0) * xst + (int64_t)h * (kv ? dst.vsh : dst.ksh) + e;
-    codes = (kv ? c.v : c.k) + ((int64_t)cap0 + p + r0) * cst + (int64_t)h * (kv ? c.vsh : c.ksh) + e;
-    scales = (kv ? c.vs : c.ks) + (int64_t)((cap0 >> c.shift) + b) * c.Hkv + h;
-  }
-  __device__ __forceinline__ void go_on() { x += dx; codes += dc; }
-};
+// 8 floats to a 32-byte boundary in one piece: a warp's store covers whole sectors, not one half of each after the other.
+__device__ __forceinline__ void store32(float* p, const float* x) {
+  asm volatile("st.global.v8.f32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+               ::"l"(p), "f"(x[0]), "f"(x[1]), "f"(x[2]), "f"(x[3]), "f"(x[4]), "f"(x[5]), "f"(x[6]), "f"(x[7]) : "memory");
+}
 
-constexpr int kReadBlocks = 4;           // per SM
-
-template <typename T, int D, int CODE>
-__global__ void __launch_bounds__(kCThreads, kReadBlocks)
-cache_read_kernel(CacheRows dst, const int32_t* __restrict__ starts, DamCacheView c, uint32_t slots, uint32_t* __restrict__ scratch) {
+// A read's slot is 2^shift packed tokens of a sequence, all heads of K or of V: up to kRPieces pieces of 8 elements, which lie one after
+// the other in memory where the rows are dense, however many heads share a row (a slot of one head left every other head's bytes of
+// a row to another block: 128k fp32 tokens of 4 heads of 64, 64 us instead of 58; 64 short reads 7.2 instead of 4.1).  Tokens of more pieces than that are cut into `cuts`.
+// DENSE: codes and rows are [token][head][d] without gaps, and fp32 rows begin on a 32-byte boundary.  grid: (slot, K or V, cut), the cut fastest.
+template <typename T, int D, int CODE, bool DENSE>
+__global__ void __launch_bounds__(kRThreads, kRBlocks)
+cache_read_kernel(CacheRows dst, const int32_t* __restrict__ starts, DamCacheView c, uint32_t slots, int shift, uint32_t cuts,
+                  uint32_t* __restrict__ scratch) {
   dam_chain_prologue();
-  constexpr int TPR = D / 8, RPP = kCThreads / TPR, PASSES = kReadTokens / RPP;
   if (blockIdx.x == 0) report_ranges(c, dst.cu, starts, scratch);
-  const int r0 = threadIdx.x / TPR;
-  Slots<ReadSlot<T, D>> it(c);
-  uint2 v[PASSES], w[PASSES];
-  float s[PASSES], z[PASSES];
-  auto load = [&](const ReadSlot<T, D>& y, uint2* r, float* f) {
+  const uint32_t side = blockIdx.x / cuts, cut = blockIdx.x - side * cuts, step = gridDim.x / (2 * cuts);
+  const bool kv = side & 1u;
+  uint32_t slot = side >> 1, until = 0u;                     // until: first slot of the next sequence
+  const int64_t xst = kv ? dst.vst : dst.kst, cst = kv ? c.vst : c.kst;
+  T* const X = reinterpret_cast<T*>(const_cast<void*>(kv ? dst.V : dst.K));
+  const unsigned char* const C = kv ? c.v : c.k;
+  const float* const S = kv ? c.vs : c.ks;
+  // this thread's pieces: token of the slot (none: beyond every slot), head, and where they stand in codes and rows
+  int r[kRPasses], h[kRPasses];
+  int64_t co[kRPasses], xo[kRPasses];                        // (DENSE: known when compiled, but for a start)
+  const int64_t mine = 8 * ((int64_t)threadIdx.x + cut * kRPieces);
 #pragma unroll
-    for (int i = 0; i < PASSES; ++i) {
-      const int t = r0 + i * RPP;
-      r[i] = make_uint2(0u, 0u);                             // (a row that cannot be read: code 0 of scale 0)
-      f[i] = 0.f;
-      if (t < y.readable) {
-        r[i] = __ldcs(reinterpret_cast<const uint2*>(y.codes + i * RPP * y.cst));
-        f[i] = __ldg(y.scales + (int64_t)((y.p + t) >> c.shift) * c.Hkv);
+  for (int i = 0; i < kRPasses; ++i) {
+    const int per = c.Hkv * (D / 8), f = (int)threadIdx.x + kRThreads * i + (int)cut * kRPieces;
+    r[i] = f / per;
+    const int piece = f - r[i] * per, e = piece % (D / 8) * 8;
+    h[i] = piece / (D / 8);
+    co[i] = DENSE ? 8 * kRThreads * i : r[i] * cst + h[i] * (kv ? c.vsh : c.ksh) + e;
+    xo[i] = DENSE ? 8 * kRThreads * i : r[i] * xst + h[i] * (kv ? dst.vsh : dst.ksh) + e;
+    if (r[i] >> shift) r[i] = 0x7FFFFFFF;
+  }
+  int b = 0, t0 = 0, cap0 = 0, start = 0, all = 0, zero = 0;  // the sequence of the slot: see WriteSlot; `all`: its tokens
+  bool fits = false;
+  // the present slot: its first token's place among `all`, and the tokens from it on
+  int base = 0;
+  auto seek = [&]() -> bool {
+    for (; slot < slots; slot += step) {
+      if (slot >= until) {
+        b = cache_seq_of_slot(dst.cu, c.num_seqs, shift, 1, slot);
+        t0 = __ldg(dst.cu + b);
+        cap0 = __ldg(c.cu + b);
+        const int t1 = __ldg(dst.cu + b + 1);
+        all = t1 - t0;
+        fits = range_fits(c, starts, b, all, &start);
+        zero = (t0 >> shift) + b;
+        until = (uint32_t)(t1 >> shift) + (uint32_t)(b + 1);
+      }
+      const int64_t at = (int64_t)((int)slot - zero) << shift;
+      if (at < all) {
+        base = (int)at;
+        return true;
+      }
+    }
+    return false;
+  };
+  uint2 v[kRPasses], w[kRPasses];
+  float s[kRPasses], z[kRPasses];
+  auto load = [&](uint2* to, float* scale) {
+    const unsigned char* codes = C + ((int64_t)cap0 + start + base) * cst + (DENSE ? mine : 0);
+    const float* scales = S + (int64_t)((cap0 >> c.shift) + b) * c.Hkv;
+#pragma unroll
+    for (int i = 0; i < kRPasses; ++i) {
+      to[i] = make_uint2(0u, 0u);                            // (a sequence that cannot be read: code 0 of scale 0)
+      scale[i] = 0.f;
+      if (fits && r[i] < all - base) {
+        to[i] = __ldcs(reinterpret_cast<const uint2*>(codes + co[i]));
+        scale[i] = __ldg(scales + (int64_t)((start + base + r[i]) >> c.shift) * c.Hkv + h[i]);
       }
     }
   };
-  bool have = it.seek(c, dst, starts, slots);
-  if (have) load(it.at, v, s);
+  bool have = seek();
+  if (have) load(v, s);
   while (have) {
-    T* const x = it.at.x;
-    const int64_t xst = it.at.xst;
-    const int n = it.at.n;
-    have = it.next(c, dst, starts, slots);
-    if (have) load(it.at, w, z);
+    // the next slot's codes are on their way while this one's values are written
+    T* const x = X + ((int64_t)t0 + base) * xst + (DENSE ? mine : 0);
+    const int n = all - base;
+    slot += step;
+    have = seek();
+    if (have) load(w, z);
 #pragma unroll
-    for (int i = 0; i < PASSES; ++i) {
+    for (int i = 0; i < kRPasses; ++i) {
       float f[8];
       code_values<CODE>(v[i].x, s[i], f);
       code_values<CODE>(v[i].y, s[i], f + 4);
-      if (r0 + i * RPP < n) Eight<T>::store(x + i * RPP * xst, f);
+      if (r[i] < n) {
+        if constexpr (DENSE && sizeof(T) == 4) store32(x + xo[i], f);
+        else Eight<T>::store(x + xo[i], f);
+      }
     }
 #pragma unroll
-    for (int i = 0; i < PASSES; ++i) { v[i] = w[i]; s[i] = z[i]; }
+    for (int i = 0; i < kRPasses; ++i) { v[i] = w[i]; s[i] = z[i]; }
   }
 }
 
@@ -440,10 +452,20 @@ cudaError_t launch_write(const CacheRows& src, const int32_t* starts, const DamC
 }
 
 template <typename T, int D, int CODE>
-cudaError_t launch_read(const CacheRows& dst, const int32_t* starts, const DamCacheView& c, int64_t slots, int sms, uint32_t* scratch,
+cudaError_t launch_read(const CacheRows& dst, const int32_t* starts, const DamCacheView& c, int64_t tokens, int sms, uint32_t* scratch,
                         cudaStream_t st) {
-  return dam_launch_chained(cache_read_kernel<T, D, CODE>, dim3(slot_grid(slots, c, sms * kReadBlocks)), dim3(kCThreads), 0, st, dst, starts, c,
-                            (uint32_t)slots, scratch);
+  // as many tokens as have kRPieces pieces, at most 64; one token of more pieces is cut
+  const int64_t per = (int64_t)c.Hkv * (D / 8), cuts = (per + kRPieces - 1) / kRPieces;
+  int shift = 0;
+  while (shift < 6 && (per << (shift + 1)) <= kRPieces) ++shift;
+  const int64_t slots = (tokens >> shift) + c.num_seqs, at_once = (int64_t)sms * kRBlocks / (2 * cuts);
+  const int64_t grid = 2 * cuts * (slots < at_once ? slots : at_once > 0 ? at_once : 1);
+  if (slots > 0x3FFFFFFF || per > 0x3FFFFFFF || grid > 0x7FFFFFFF) return cudaErrorNotSupported;
+  auto dense = [&](int64_t st, int64_t sh) { return sh == D && st == (int64_t)c.Hkv * D; };
+  const bool aligned = sizeof(T) == 2 || (reinterpret_cast<uintptr_t>(dst.K) | reinterpret_cast<uintptr_t>(dst.V)) % 32 == 0;
+  const bool all = aligned && dense(dst.kst, dst.ksh) && dense(dst.vst, dst.vsh) && dense(c.kst, c.ksh) && dense(c.vst, c.vsh);
+  return dam_launch_chained(all ? cache_read_kernel<T, D, CODE, true> : cache_read_kernel<T, D, CODE, false>, dim3((unsigned)grid), dim3(kRThreads), 0, st, dst, starts, c, (uint32_t)slots, shift,
+                            (uint32_t)cuts, scratch);
 }
 
 cudaError_t sm_count(int* sms) {
@@ -477,8 +499,6 @@ cudaError_t dam_launch_cache_read(const dam_cache_t* cache, const dam_shape_t* t
   int sms = 0;
   const cudaError_t e = sm_count(&sms);
   if (e != cudaSuccess) return e;
-  const int64_t slots = tokens->total_tokens / kReadTokens + (int64_t)c.num_seqs;
-  if (slots * 2 * c.Hkv > 0x7FFFFFFF) return cudaErrorNotSupported;
-  return DAM_CACHE_DISPATCH(launch_read, tokens->dtype, tokens->head_dim, cache->code, rows_of(K, V, tokens), starts, c, slots, sms,
-                            reinterpret_cast<uint32_t*>(scratch), st);
+  return DAM_CACHE_DISPATCH(launch_read, tokens->dtype, tokens->head_dim, cache->code, rows_of(K, V, tokens), starts, c,
+                            (int64_t)tokens->total_tokens, sms, reinterpret_cast<uint32_t*>(scratch), st);
 }

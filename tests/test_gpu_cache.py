@@ -157,6 +157,22 @@ def test_rows_with_strides_and_codes_by_head():
     assert (other[:, 3:] == 7).all()
 
 
+@pytest.mark.parametrize("Hkv,d,dtype,offset", [(1, 64, F32, 4), (3, 128, F32, 0), (64, 128, BF16, 0), (130, 64, BF16, 8), (70, 128, F32, 0)])
+def test_reads_of_any_number_of_heads_and_of_rows_off_the_widest_boundary(Hkv, d, dtype, offset):
+    """Tokens of a few pieces and tokens that a slot cannot hold; rows that begin 16 bytes behind a 32-byte boundary."""
+    rng = np.random.default_rng(15)
+    p = _filled(rng, [70, 33], Hkv, d, "int8", 16, dtype)
+    tokens = B.make_shape([0, 40, 73], Hkv, Hkv, d, dtype, DEV)
+    whole = [torch.full((73 * Hkv * d + 2 * offset + 8,), 5.0, dtype=dtype, device=DEV) for _ in range(2)]
+    K, V = (x[offset:offset + 73 * Hkv * d].view(73, Hkv, d) for x in whole)
+    _, _, scratch = B.dam_cache_read(p.cache, tokens, _ints([30, 0]), K, V)
+    assert B.dam_poll_status(scratch) == 0
+    for got, side, x in ((K, p.k, whole[0]), (V, p.v, whole[1])):
+        want = torch.from_numpy(np.concatenate([side[0].read(30, 40), side[1].read(0, 33)])).to(dtype)
+        assert torch.equal(got.cpu(), want)
+        assert (x[:offset] == 5).all() and (x[offset + got.numel():] == 5).all()
+
+
 def test_ranges_outside_the_capacity_are_refused_alone():
     rng = np.random.default_rng(11)
     p = Pair([64, 64, 64, 64], 1, 64, "e4m3", 16, BF16)
