@@ -5,7 +5,9 @@
 // registers from the one time they are read, finds their largest magnitude, and writes the codes; nothing is read twice.
 // Where the block of tokens was begun by an earlier call its scale can only grow, and when it does the tokens that are
 // there are read back and quantised again.  Read: value = code * scale.  Both move bytes and do little else: HBM bounds them
-// (2 + 1 bytes per element of a bf16 write, 1 + 2 of a read).
+// (2 + 1 bytes per element of a bf16 write, 1 + 2 of a read; 128k tokens of 8 KV heads of 128, 805 MB either way: written in 133 us,
+// read in 131, 6.0 and 6.1 TB/s), once the instructions per element are few enough (two fused multiply-adds that enclose the
+// quotient instead of a division or a rounding instruction: the first form of the write took 240 us).
 #include <type_traits>
 
 #include "dam_cache.cuh"
