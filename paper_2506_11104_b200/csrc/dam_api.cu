@@ -278,7 +278,7 @@ cudaError_t dam_current_device(int* device, DamDeviceInfo* info) {
 
 extern "C" {
 
-int32_t dam_version(void) { return 1001; }
+int32_t dam_version(void) { return 1002; }
 
 const char* dam_status_string(dam_status_t s) {
   switch (s) {

@@ -8,7 +8,8 @@
 // instruction's tile, so nothing of it is padding where a group has 8 heads.  fp16 operands: q is scaled by a power of two so
 // that its largest element lies in [2^14, 2^15) (a bf16 q is then exact wherever it matters), the probabilities are taken
 // relative to a running maximum times sV over a running reference, at most 2^15.  An fp32 q and its probabilities are each the
-// sum of two fp16 numbers (22 bits), at the price of twice the instructions.
+// sum of two fp16 numbers (22 bits), at the price of twice the instructions.  What fp16's last step of 2^-24 drops of a weight is
+// 2^-31 of the largest V a scale can stand for, in either type.
 //
 // A warp works on slices of 16 keys (two at a time where keys are contiguous: two independent chains of instructions), brought to
 // shared memory by asynchronous copies ahead of their use, and keeps a running softmax and its share of O^T of its own; the warps of

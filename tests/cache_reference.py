@@ -107,14 +107,15 @@ def tolerance(O, A, S, vmax, n, dtype):
     """How far O [d] may be off.  With A, S, vmax, n as above and u = 2^-24:
       logits     d products and sums in fp32 and three more roundings, a tensor-core sum rounded toward zero (2 u each): off by
                  (2 d + 8) u S + 2^-21 (exponential), twice that in O relative to A (numerator and denominator)
-      weights    held as fp16 (2^-11 relative), or as two of them (2^-22); below fp16's normal range off by 2^-25 of a unit that is
-                 at most vmax / 64: n 2^-31 vmax (2^-42 with two)
+      weights    held as fp16 (2^-11 relative), or as the sum of two (2^-22); the step of fp16 below its normal range is 2^-24, and
+                 neither one number nor the second of two is finer: off by 2^-25 of a unit that is at most vmax / 64 (the reference
+                 keeps the largest weight of a scale above 64): n 2^-31 vmax
       sums       n / 16 tensor-core sums of 16 products, 2 u each, and the joining of warps and blocks, relative to A
       result     rounded once"""
     u, d = 2.0 ** -24, O.shape[0]
     bf16 = dtype == torch.bfloat16
     rel = 2 * ((2 * d + 8) * u * S + 2.0 ** -21) + (2.0 ** -11 if bf16 else 2.0 ** -22) + 2 * u * (n / 16 + 32)
-    return rel * A + n * vmax * (2.0 ** -31 if bf16 else 2.0 ** -42) + np.abs(O) * (2.0 ** -8 if bf16 else u)
+    return rel * A + n * vmax * 2.0 ** -31 + np.abs(O) * (2.0 ** -8 if bf16 else u)
 
 
 def lse_tolerance(lse, d, S, n):
