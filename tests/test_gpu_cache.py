@@ -541,3 +541,83 @@ def test_prompt_chunk_and_generation_together():
         assert torch.equal(torch.isfinite(lse[:, i]), fin)
         bound = 4 * 2.0 ** -8 * float(Vc.float().abs().max())
         assert (o[0].float() - O[i].float()).abs().max() <= bound
+
+
+@pytest.mark.parametrize("d,long", [(128, 4500000), (64, 70000)])
+def test_offsets_beyond_32_bits(d, long):
+    """A second sequence whose codes begin more than 2^32 bytes into the cache (by its length, or by the stride of a token)."""
+    rng = np.random.default_rng(43)
+    Hkv, Hq, lengths = (8, 16, [long, 700]) if d == 128 else (1, 2, [long, 700])
+    T = sum(lengths)
+    if d == 128:
+        codes = [torch.zeros(T, Hkv, d, dtype=torch.int8, device=DEV) for _ in range(2)]
+    else:                                                     # 64 bytes of every 65536
+        codes = [torch.zeros(T, 65536, dtype=torch.int8, device=DEV)[:, None, 128:192] for _ in range(2)]
+    assert (long * codes[0].stride(0)) > 2 ** 32
+    cache = B.make_cache(_cu(lengths), Hkv, d, "int8", 64, DEV, *codes)
+    xs = [_rows(rng, 300 + 500, Hkv, d, BF16) for _ in range(2)]
+    tokens = B.make_shape([0, 300, 800], Hkv, Hkv, d, BF16, DEV)
+    starts = _ints([long - 300, 0])
+    assert B.dam_poll_status(B.dam_cache_write(xs[0], xs[1], tokens, cache, starts)) == 0
+    sides = []
+    for x, scales in zip(xs, (cache.k_scales, cache.v_scales)):
+        tail, head = R.Side(300 + long % 64, Hkv, d, "int8", 64), R.Side(700, Hkv, d, "int8", 64)
+        begun = (long - 300) % 64                             # (the block it begins in was begun before, with the scale 0 of the zeros)
+        tail = R.Side(begun + 300, Hkv, d, "int8", 64)
+        tail.write(x[:300].cpu().double().numpy(), begun)
+        head.write(x[300:].cpu().double().numpy(), 0)
+        sides.append((tail, head, begun))
+    K, V, scratch = B.dam_cache_read(cache, tokens, starts)
+    assert B.dam_poll_status(scratch) == 0
+    for got, (tail, head, begun) in zip((K, V), sides):
+        want = torch.from_numpy(np.concatenate([tail.read(begun, 300), head.read(0, 500)])).to(BF16)
+        assert torch.equal(got.cpu(), want)
+    p = Pair.__new__(Pair)
+    p.Hkv, p.d, p.dtype = Hkv, d, BF16
+    p.k, p.v = [sides[0][1]], [sides[1][1]]
+    q = torch.from_numpy(rng.standard_normal((2, Hq, d))).float().to(BF16).to(DEV)
+    blob, keep = _blob(rng, [100, 100], Hq, 64)
+    for mask in (None, blob):
+        O, lse, scratch = B.dam_cache_decode_attention(q, cache, _ints([0, 499]), mask)
+        assert B.dam_poll_status(scratch) == 0
+        _check(p, q[1:], [499], O[1:], lse[1:], mask is not None and (lambda b, h, i: keep(1, h, i)) or None, heads=[0, Hq - 1])
+    # the far end of the first sequence, under patterns that reach its last keys only
+    L = 64
+    P = np.zeros((2, Hq, L, L), np.float32)
+    for r in range(40):
+        P[:, :, np.arange(r, L), np.arange(0, L - r)] = 1
+    shape = B.make_shape([0, 100, 200], Hq, Hkv, d, BF16, DEV)
+    blob, _ = B.dam_build_masks_from_scores(torch.from_numpy(P.reshape(-1)).to(DEV), shape, B.make_rule(L, 0.3, 1.0))
+    O, lse, scratch = B.dam_cache_decode_attention(q, cache, _ints([long - 1, 499]), blob)
+    assert B.dam_poll_status(scratch) == 0
+    D, _, cols = B.MaskBlob(blob).pattern_bits(0, 0)
+    near = np.flatnonzero(D)
+    assert near.max() < 300
+    tail_k, tail_v, begun = sides[0][0], sides[1][0], sides[0][2]
+    at = sorted(begun + 299 - near)
+    Kt, Vt = tail_k.values(begun + 300)[at], tail_v.values(begun + 300)[at]
+    Kt, Vt = (np.concatenate([np.zeros((int(cols.sum()), Hkv, d)), x]) for x in (Kt, Vt))   # (the sequence begins with zeros)
+    for h in (0, Hq - 1):
+        g = h // (Hq // Hkv)
+        want, want_l, A, S, vmax, n = R.attention(q[0, h].cpu().double().numpy(), Kt[:, g], Vt[:, g], np.ones(len(Kt), bool), 1 / math.sqrt(d))
+        assert (np.abs(O[0, h].cpu().double().numpy() - want) <= R.tolerance(want, A, S, vmax, n, BF16)).all()
+        assert abs(float(lse[0, h]) - want_l) <= R.lse_tolerance(want_l, d, S, n)
+
+
+def test_two_streams_at_once():
+    """Two caches, two streams, calls interleaved: what each gets alone."""
+    rng = np.random.default_rng(45)
+    caches = [_filled(rng, [3000, 40], 2, 128, "int8", 64, BF16), _filled(rng, [700] * 90, 2, 64, "e4m3", 16, BF16)]
+    qs = [torch.from_numpy(rng.standard_normal((n, 8, d))).float().to(BF16).to(DEV) for n, d in ((2, 128), (90, 64))]
+    pos = [_ints([2999, 39]), _ints([699] * 90)]
+    want = [B.dam_cache_decode_attention(q, p.cache, x)[:2] for q, p, x in zip(qs, caches, pos)]
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    torch.cuda.synchronize()
+    got = [[], []]
+    for _ in range(20):
+        for k in range(2):
+            with torch.cuda.stream(streams[k]):
+                got[k].append(B.dam_cache_decode_attention(qs[k], caches[k].cache, pos[k])[:2])
+    torch.cuda.synchronize()
+    for k in range(2):
+        assert all(torch.equal(o, want[k][0]) and torch.equal(l, want[k][1]) for o, l in got[k])
