@@ -481,25 +481,28 @@ struct CacheDecode {
 // Where a share ends inside a sequence's keys it leaves a partial result, and a second kernel joins those.
 constexpr int kMaxShares = 148;        // blocks: one per SM of a B200
 
+// (EARLY: of the joining kernel, before it waits for the one before it: past the L1 cache, whose lines may be older than that wait)
+template <bool EARLY = false>
 __device__ __forceinline__ int chunks_of(const DamCacheView& c, const int32_t* pos, int b, int chunk) {
-  const int p = __ldg(pos + b), room = __ldg(c.cu + b + 1) - __ldg(c.cu + b);
+  const int p = EARLY ? __ldcg(pos + b) : __ldg(pos + b), room = __ldg(c.cu + b + 1) - __ldg(c.cu + b);
   return (unsigned)p >= (unsigned)room ? 0 : p / chunk + 1;
 }
 
 constexpr int kKeys = kTile * kSlice;    // keys of a warp's tile
 
 // Chunks per head of all sequences, of those before sequence b, and whether some position lies outside its capacity (whole warp).
+template <bool EARLY = false>
 struct Survey {
   int total, before, mine;     // mine: chunks of sequence `lane`
   bool bad;
   __device__ __forceinline__ Survey(const DamCacheView& c, const int32_t* pos, int chunk, int b) : bad(false) {
     const int lane = threadIdx.x & 31;
-    mine = lane < c.num_seqs ? chunks_of(c, pos, lane, chunk) : 0;
+    mine = lane < c.num_seqs ? chunks_of<EARLY>(c, pos, lane, chunk) : 0;
     bad = lane < c.num_seqs && mine == 0;
     total = mine;
     before = lane < b ? mine : 0;
     for (int x = 32 + lane; x < c.num_seqs; x += 32) {
-      const int n = chunks_of(c, pos, x, chunk);
+      const int n = chunks_of<EARLY>(c, pos, x, chunk);
       bad |= n == 0;
       total += n;
       before += x < b ? n : 0;
@@ -520,7 +523,7 @@ struct Place {
     live = __ldg(pos + b) + 1 - k * chunk - (int)(threadIdx.x >> 5) * kKeys;
   }
   // chunk `at` of the whole list (which has it); returns its number within the (KV head, group)
-  __device__ __forceinline__ int locate(const DamCacheView& c, const int32_t* pos, const Survey& all, int chunk, int heads, int at) {
+  __device__ __forceinline__ int locate(const DamCacheView& c, const int32_t* pos, const Survey<>& all, int chunk, int heads, int at) {
     const int lane = threadIdx.x & 31;
     int before = 0, mine = all.mine;
     b = hg = 0; n = left = 1; live = 0;
@@ -621,7 +624,7 @@ cache_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_const
   // The joining kernel may begin when this one has seen its predecessors' memory: it reads the positions before it waits for this.
   asm volatile("griddepcontrol.wait;" ::: "memory");
   asm volatile("griddepcontrol.launch_dependents;");
-  const Survey all(c, a.pos, LY::chunk, 0);
+  const Survey<> all(c, a.pos, LY::chunk, 0);
   // sequences whose position lies outside their capacity get zeros; block 0 says so in the status word
   if (blockIdx.x == 0 && tid < 64) a.scratch[tid] = tid == 1 && all.bad ? (uint32_t)DAM_ERR_INVALID_ARGUMENT : 0u;
   if (all.bad) {
@@ -757,8 +760,8 @@ cache_join_kernel(CacheDecode a, DamCacheView c, const float* __restrict__ parti
   const int g = blockIdx.x % per, hg = blockIdx.x / per % heads, b = blockIdx.x / per / heads;
   const int sub = hg % a.NS, nh = min(kGMaxGroup, a.G - sub * kGMaxGroup);
   const int tid = threadIdx.x, way = tid / TD, col = tid % TD;
-  const int n = chunks_of(c, a.pos, b, chunk);
-  const Survey all(c, a.pos, chunk, b);
+  const int n = chunks_of<true>(c, a.pos, b, chunk);
+  const Survey<true> all(c, a.pos, chunk, b);
   const int list = a.side > 1 ? 1 : heads;
   const Shares sh(max(all.total * list, 1), shares);
   const int first = all.before * list + (a.side > 1 ? 0 : hg * n), s0 = sh.of(first), s1 = n ? sh.of(first + n - 1) : s0;
