@@ -318,7 +318,8 @@ dam_status_t dam_cache_sizes(const dam_cache_t* cache, int32_t num_q_heads, size
  * A block whose first token is among the new ones gets its scale from the new ones. A block that was begun before keeps its
  * scale, or gets the larger one that its new tokens want; then the tokens that stand before starts[b] in it are read back (a
  * float) and quantised again. Tokens behind the last new one are left as they are: they no longer belong to the sequence.
- *   K, V    : DEVICE, 16-byte aligned.   starts_dev : DEVICE, int32[num_seqs], or NULL: every sequence from token 0.
+ *   K, V    : DEVICE, 16-byte aligned (NULL will do where no sequence gets a token).
+ *   starts_dev : DEVICE, int32[num_seqs], or NULL: every sequence from token 0.
  *   scratch : DEVICE, >= 256 bytes, 256-byte aligned. A sequence whose tokens do not fit its capacity (starts[b] < 0 or
  *             starts[b] + tokens > capacity) is left alone and gives INVALID_ARGUMENT in the status word.
  * The new rows must not lie inside the cache. Errors: INVALID_ARGUMENT, UNSUPPORTED (head_dim), BUFFER_TOO_SMALL, CUDA.

@@ -7,7 +7,6 @@ fails, an exception is raised.
 from __future__ import annotations
 
 import ctypes
-import functools
 import os
 from dataclasses import dataclass
 from typing import List, Optional, Sequence
@@ -134,17 +133,22 @@ def _stream(device) -> int:
     return _raw_stream(index)
 
 
+class _ByReference:
+    """`ref` is the reference to the structure `c`, made when c is set (every call passes it; byref takes as long as a check)."""
+
+    def __setattr__(self, name, value):
+        object.__setattr__(self, name, value)
+        if name == "c":
+            object.__setattr__(self, "ref", ctypes.byref(value))
+
+
 @dataclass
-class Shape:
+class Shape(_ByReference):
     """Python-side owner of a dam_shape_t and the cu_seqlens buffers it points to."""
     c: dam_shape_t
     cu_host: np.ndarray
     cu_dev: Optional[torch.Tensor]
     lengths: List[int]
-
-    @functools.cached_property
-    def ref(self):
-        return ctypes.byref(self.c)
 
 
 def make_shape(cu_seqlens: Sequence[int], Hq: int, Hkv: int, d: int, dtype: torch.dtype, device=None,
@@ -353,7 +357,7 @@ CACHE_CODES = {"int8": (0, torch.int8), "e4m3": (1, torch.float8_e4m3fn)}
 
 
 @dataclass
-class Cache:
+class Cache(_ByReference):
     """Python-side owner of a dam_cache_t and the buffers it points to."""
     c: dam_cache_t
     cu_host: np.ndarray
@@ -365,10 +369,6 @@ class Cache:
     v_scales: Optional[torch.Tensor]
     num_seqs: int                # (as in c; a field of a ctypes structure takes several times as long to read)
     head_dim: int
-
-    @functools.cached_property
-    def ref(self):
-        return ctypes.byref(self.c)
 
 
 def make_cache(cu_seqlens: Sequence[int], Hkv: int, d: int, code: str = "int8", block_tokens: int = 64, device=None,
@@ -414,8 +414,10 @@ def dam_cache_sizes(cache: Cache, Hq: int):
 
 
 def _per_sequence(x: torch.Tensor, n: int) -> int:
-    """Pointer of an int32 tensor with one element per sequence."""
+    """Pointer of an int32 tensor on the device with one element per sequence."""
     assert x.dtype is torch.int32 and x.numel() == n and x.is_contiguous()
+    if not x.is_cuda:
+        raise ValueError("one number per sequence, on the device: got a tensor of " + str(x.device))
     return x.data_ptr()
 
 

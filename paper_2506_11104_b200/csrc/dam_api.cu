@@ -485,8 +485,9 @@ dam_status_t check_cache_rows(const dam_cache_t* cache, const dam_shape_t* token
   if ((st = check_cache(cache, true)) != DAM_OK) return st;
   if (tokens->num_seqs != cache->num_seqs || tokens->num_kv_heads != cache->num_kv_heads || tokens->head_dim != cache->head_dim)
     return DAM_ERR_INVALID_ARGUMENT;
-  if (!K || !V || !scratch || !aligned(K, 16) || !aligned(V, 16) || !aligned(scratch, 256) || (starts_dev && !aligned(starts_dev, 4)))
-    return DAM_ERR_INVALID_ARGUMENT;
+  // (a tensor without rows has no address; a call without tokens touches none)
+  if (tokens->total_tokens > 0 && (!K || !V)) return DAM_ERR_INVALID_ARGUMENT;
+  if (!scratch || !aligned(K, 16) || !aligned(V, 16) || !aligned(scratch, 256) || !aligned(starts_dev, 4)) return DAM_ERR_INVALID_ARGUMENT;
   if (tokens->total_tokens > 0x7FFFFFFF - 255) return DAM_ERR_INVALID_ARGUMENT;
   return scratch_bytes < 256 ? DAM_ERR_BUFFER_TOO_SMALL : DAM_OK;
 }

@@ -135,6 +135,34 @@ def test_bad_calls_are_refused():
     assert lib.dam_cache_sizes(c.ref, 8, None, None) == 0
 
 
+def test_a_call_without_tokens_needs_no_rows():
+    """(The address of a tensor without rows is NULL.)"""
+    lib, c = B.lib(), _cache()
+    none = B.make_shape([0, 0, 0, 0], 8, 2, 128, torch.bfloat16)
+    assert lib.dam_cache_write(None, None, none.ref, 0x1000, c.ref, 0x1000, 255, None) == 3          # the scratch is all that is wrong
+    assert lib.dam_cache_read(c.ref, none.ref, 0x1000, None, None, 0x1000, 255, None) == 3
+
+
+def test_the_reference_follows_the_structure():
+    shape, cache = B.make_shape([0, 64], 2, 1, 64, torch.bfloat16), B.make_cache([0, 64], 1, 64)
+    assert B.dam_cache_sizes(cache, 2)[0] == 2
+    shape.c, cache.c = B.make_shape([0, 96], 2, 1, 64, torch.bfloat16).c, B.make_cache([0, 128], 1, 64).c
+    assert B.dam_cache_sizes(cache, 2)[0] == 3
+    assert shape.ref._obj is shape.c and cache.ref._obj is cache.c
+
+
+def test_starts_and_positions_in_host_memory_are_refused():
+    """Where every other tensor is on a device (one without memory here)."""
+    cache = B.make_cache([0, 64], 1, 64, "e4m3", 16, "cpu")
+    shape = B.make_shape([0, 64], 2, 1, 64, torch.bfloat16, "cpu")
+    x, i = torch.zeros(64, 1, 64, dtype=torch.bfloat16, device="meta"), torch.zeros(1, dtype=torch.int32)
+    buf = torch.zeros(1 << 22, dtype=torch.uint8)
+    for call in (lambda: B.dam_cache_write(x, x, shape, cache, i, buf), lambda: B.dam_cache_read(cache, shape, i, x, x, buf),
+                 lambda: B.dam_cache_decode_attention(x[:2].view(1, 2, 64), cache, i, None, 0.0, x, x, buf)):
+        with pytest.raises(ValueError, match="on the device"):
+            call()
+
+
 def test_host_tensors_are_refused():
     cache = B.make_cache([0, 64], 1, 64, "e4m3", 16, "cpu")
     shape = B.make_shape([0, 64], 2, 1, 64, torch.bfloat16, "cpu")

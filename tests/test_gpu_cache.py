@@ -621,3 +621,43 @@ def test_two_streams_at_once():
     torch.cuda.synchronize()
     for k in range(2):
         assert all(torch.equal(o, want[k][0]) and torch.equal(l, want[k][1]) for o, l in got[k])
+
+
+def test_calls_without_tokens():
+    """No sequence gets a token: nothing is written or read, whatever the starts, and the status says so."""
+    rng = np.random.default_rng(46)
+    p = _filled(rng, [40, 70], 2, 64, "int8", 16, BF16)
+    none = torch.empty(0, 2, 64, dtype=BF16, device=DEV)
+    tokens = B.make_shape([0, 0, 0], 2, 2, 64, BF16, DEV)
+    for starts in (None, _ints([0, 70]), _ints([-5, 1 << 30])):
+        assert B.dam_poll_status(B.dam_cache_write(none, none, tokens, p.cache, starts)) == 0
+        K, V, scratch = B.dam_cache_read(p.cache, tokens, starts)
+        assert K.shape == V.shape == (0, 2, 64) and B.dam_poll_status(scratch) == 0
+    p.check()
+
+
+def test_a_long_sequence_captured_and_replayed_at_other_positions():
+    """The list form and its join, replayed while the positions move over the bounds of the shares."""
+    rng = np.random.default_rng(47)
+    lengths = [70000, 300]
+    p = _filled(rng, lengths, 1, 64, "int8", 64, BF16)
+    q = torch.from_numpy(rng.standard_normal((2, 4, 64))).float().to(BF16).to(DEV)
+    pos, O, lse = _ints([0, 0]), torch.zeros_like(q), torch.zeros(2, 4, device=DEV)
+    scratch = torch.empty(B.dam_cache_sizes(p.cache, 4)[1], dtype=torch.uint8, device=DEV)
+    B.dam_cache_decode_attention(q, p.cache, pos, O=O, lse=lse, scratch=scratch)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        pos.add_(1)
+        B.dam_cache_decode_attention(q, p.cache, pos, O=O, lse=lse, scratch=scratch)
+    for at in ([0, 298], [511, 0], [1022, 100], [40000, 7], [69996, 200]):
+        pos.copy_(_ints(at))
+        for step in range(3):
+            g.replay()
+            got = O.clone(), lse.clone()
+            eager = B.dam_cache_decode_attention(q, p.cache, pos.clone())
+            inside = [k for k in range(2) if at[k] + 1 + step < lengths[k]]
+            assert B.dam_poll_status(scratch) == (0 if len(inside) == 2 else 1)
+            assert torch.equal(got[0], eager[0]) and torch.equal(got[1], eager[1])
+            if len(inside) == 2:
+                _check(p, q, [x + 1 + step for x in at], *got)
