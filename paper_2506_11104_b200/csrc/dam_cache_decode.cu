@@ -34,6 +34,7 @@ constexpr int kSlice = 16;             // keys of a slice: the rows of the first
 constexpr int kTile = 2;               // slices that a warp takes at a time where the keys are contiguous: two independent chains
 
 constexpr int kGMaxGroup = 8;         // query heads a block takes: the narrow side of the instructions' tiles
+constexpr int kPackGroup = 4;         // so many at most, and both numbers of an fp32 value fit into it
 
 __device__ __forceinline__ float g_ex2(float x) {
   float y;
@@ -132,9 +133,13 @@ struct Rows {
 // What a warp carries through the keys of one (sequence, up to 8 query heads of one KV head).  Lane = 4 row + quad: the lane
 // holds the logits of keys row and row + 8 against heads 2 quad and 2 quad + 1, and of O^T the dimensions D / 8 * row ... of the
 // same two heads.
-template <typename T, int D, int CODE>
+// PACK: of an fp32 q of at most four heads, the second numbers of q and P are columns 4 to 7 of the tiles; quads 2 and 3 stand for the
+// heads of quads 0 and 1 then (six sequences of 16 heads over 4 KV heads of 64: 20.9 us with two instructions each).
+template <typename T, int D, int CODE, bool PACK>
 struct WarpState {
-  static constexpr bool kSplit = sizeof(T) == 4;             // q and P as two fp16 numbers each
+  static_assert(!PACK || sizeof(T) == 4, "one number has no second");
+  static constexpr bool kSplit = sizeof(T) == 4 && !PACK;    // q and P as two fp16 numbers each, an instruction each
+  static __device__ __forceinline__ int head_of(int column) { return PACK ? column & (kPackGroup - 1) : column; }
   static constexpr int KS = D / 16;
   uint32_t qh[KS][2], ql[kSplit ? KS : 1][2];
   float qs[2];                         // logits (log2 units) per product of codes and q as it is held, of the lane's heads
@@ -154,7 +159,7 @@ struct WarpState {
   struct Query { uint4 w[D / 4 * sizeof(T) / 16]; };
   static __device__ __forceinline__ Query fetch_q(const T* q, int heads) {
     const int lane = threadIdx.x & 31, row = lane >> 2, quad = lane & 3;
-    const uint4* p = reinterpret_cast<const uint4*>(q + (int64_t)(row < heads ? row : 0) * D + D / 4 * quad);
+    const uint4* p = reinterpret_cast<const uint4*>(q + (int64_t)(head_of(row) < heads ? head_of(row) : 0) * D + D / 4 * quad);
     Query r;
 #pragma unroll
     for (int i = 0; i < (int)(sizeof(r.w) / 16); ++i) r.w[i] = __ldg(p + i);
@@ -169,7 +174,7 @@ struct WarpState {
       const uint32_t w[4] = {q.w[i].x, q.w[i].y, q.w[i].z, q.w[i].w};
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
-        if constexpr (kSplit) {
+        if constexpr (sizeof(T) == 4) {
           x[4 * i + k] = __uint_as_float(w[k]);
         } else {
           x[8 * i + 2 * k] = __uint_as_float(w[k] << 16); x[8 * i + 2 * k + 1] = __uint_as_float(w[k] & 0xFFFF0000u);
@@ -183,16 +188,18 @@ struct WarpState {
     top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
     // 2^(14 - exponent of the largest); an infinity or a NaN stays one
     const int f = min(268 - (int)(top >> 23), 253);
-    const float mul = row < heads ? __uint_as_float((uint32_t)f << 23) : 0.f;
+    const float mul = head_of(row) < heads ? __uint_as_float((uint32_t)f << 23) : 0.f;
 #pragma unroll
     for (int s = 0; s < KS; ++s) {
 #pragma unroll
       for (int k = 0; k < 2; ++k) {
         const float a = x[4 * s + 2 * k] * mul, b = x[4 * s + 2 * k + 1] * mul;
         qh[s][k] = pack_half2(a, b);
-        if constexpr (kSplit) {
+        if constexpr (kSplit || PACK) {
           const float2 hi = __half22float2(*reinterpret_cast<const __half2*>(&qh[s][k]));
-          ql[s][k] = pack_half2(a - hi.x, b - hi.y);
+          const uint32_t lo = pack_half2(a - hi.x, b - hi.y);
+          if constexpr (kSplit) ql[s][k] = lo;
+          else qh[s][k] = row < kPackGroup ? qh[s][k] : lo;
         }
       }
     }
@@ -204,7 +211,7 @@ struct WarpState {
   // N slices: rows at `rows`, scales at `sc`, and which keys there are for whom.
   //   kAll    every head keeps all of them; the 16 of a slice share their scales (they lie in one block): K's and V's, slice by slice
   //   kFirst  the same for the first `arg` keys; the rows behind may hold anything
-  //   kKeep   (one slice) bit e (e + 2) of arg: head 2 quad + e keeps key `row` (key `row + 8`), keys by Rows::key; 16 scales of K and
+  //   kKeep   (one slice) bit e (e + 2) of arg: head head_of(2 quad + e) keeps key `row` (key `row + 8`), keys by Rows::key; 16 scales of K and
   //           16 of V
   // A key that a head does not keep has no part in it.
   enum Mode { kAll, kFirst, kKeep };
@@ -253,9 +260,10 @@ struct WarpState {
 #pragma unroll
     for (int n = 0; n < N; ++n) {
 #pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        x[n][e] = kept(n, e) ? (st[n][0][e] + st[n][1][e]) * (ks[n][0] * qs[e]) : -CUDART_INF_F;
-        x[n][2 + e] = kept(n, 2 + e) ? (st[n][0][2 + e] + st[n][1][2 + e]) * (ks[n][1] * qs[e]) : -CUDART_INF_F;
+      for (int e = 0; e < 4; ++e) {
+        float y = st[n][0][e] + st[n][1][e];
+        if constexpr (PACK) y += __shfl_xor_sync(0xFFFFFFFFu, y, 2);
+        x[n][e] = kept(n, e) ? y * (ks[n][e >> 1] * qs[e & 1]) : -CUDART_INF_F;
       }
       c[n][0] = vs[n][0] * vinv;
       c[n][1] = UNIFORM ? c[n][0] : vs[n][1] * vinv;
@@ -316,7 +324,11 @@ struct WarpState {
         w[2 + e] = kept(n, 2 + e) ? p1 * c[n][1] : 0.f;
       }
       // P^T as operands (k = key, n = head): the transposes of the two 8 x 8 blocks [key][head]
-      const uint32_t h0 = pack_half2(w[0], w[1]), h1 = pack_half2(w[2], w[3]);
+      uint32_t h0 = pack_half2(w[0], w[1]), h1 = pack_half2(w[2], w[3]);
+      if constexpr (PACK) {
+        const float2 f0 = __half22float2(*reinterpret_cast<const __half2*>(&h0)), f1 = __half22float2(*reinterpret_cast<const __half2*>(&h1));
+        if (quad >= 2) { h0 = pack_half2(w[0] - f0.x, w[1] - f0.y); h1 = pack_half2(w[2] - f1.x, w[3] - f1.y); }
+      }
       pb[n][0] = movmatrix_trans(h0);
       pb[n][1] = movmatrix_trans(h1);
       if constexpr (kSplit) {
@@ -374,9 +386,16 @@ struct WarpState {
       s += __shfl_xor_sync(0xFFFFFFFFu, s, 4);
       s += __shfl_xor_sync(0xFFFFFFFFu, s, 8);
       s += __shfl_xor_sync(0xFFFFFFFFu, s, 16);
-      float* dst = mg + (2 * quad + e) * kRow;
+      float* dst = mg + (2 * quad + e) * kRow;               // (PACK: rows 4 to 7 hold copies)
 #pragma unroll
-      for (int u = 0; u < KS; ++u) *reinterpret_cast<float2*>(dst + 16 * u + 2 * row) = make_float2(o[u][e] * back, o[u][2 + e] * back);
+      for (int u = 0; u < KS; ++u) {
+        float2 y = make_float2(o[u][e] * back, o[u][2 + e] * back);
+        if constexpr (PACK) {
+          y.x += __shfl_xor_sync(0xFFFFFFFFu, y.x, 2);
+          y.y += __shfl_xor_sync(0xFFFFFFFFu, y.y, 2);
+        }
+        *reinterpret_cast<float2*>(dst + 16 * u + 2 * row) = y;
+      }
       if (row == 0) { dst[D] = m[e]; dst[D + 1] = s; }
     }
   }
@@ -598,12 +617,12 @@ __device__ __forceinline__ void drain(uint32_t bars, int stages, uint32_t phases
     if (pending >> s & 1u) sm100::mbar_wait(bars + 8 * s, phases >> s & 1u, gave_up, sm100::kDrainPolls);
 }
 
-template <typename T, int D, int CODE, int WARPS, int STAGES>
+template <typename T, int D, int CODE, bool PACK, int WARPS, int STAGES>
 __global__ void __launch_bounds__(WARPS * 32, 1)
 cache_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUtensorMap vmap, CacheDecode a, DamCacheView c,
                     float* __restrict__ partial) {
   using LY = DenseLayout<D, WARPS, STAGES>;
-  using WS = WarpState<T, D, CODE>;
+  using WS = WarpState<T, D, CODE, PACK>;
   extern __shared__ unsigned char sm_raw[];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int heads = a.side > 1 ? 1 : c.Hkv * a.NS;            // of the list
@@ -829,11 +848,11 @@ struct ShortLayout {
   static constexpr int total = flag_off + 16 + 1024;
 };
 
-template <typename T, int D, int CODE, ShortForm FORM>
+template <typename T, int D, int CODE, bool PACK, ShortForm FORM>
 __global__ void __launch_bounds__(ShortLayout<D, FORM>::warps * 32, (ShortLayout<D, FORM>::blocks))
 cache_decode_short_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUtensorMap vmap, CacheDecode a, DamCacheView c) {
   using LY = ShortLayout<D, FORM>;
-  using WS = WarpState<T, D, CODE>;
+  using WS = WarpState<T, D, CODE, PACK>;
   constexpr int WARPS = LY::warps, STAGES = LY::stages, kThreads = WARPS * 32, kChunk = WARPS * kKeys;
   extern __shared__ unsigned char sm_raw[];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -1043,12 +1062,12 @@ struct MaskedLayout {
   static constexpr int total = join_off + (CLUSTER ? ClusterJoin::bytes : 0);
 };
 
-template <typename T, int D, int CODE, bool CLUSTER>
+template <typename T, int D, int CODE, bool PACK, bool CLUSTER>
 __global__ void __launch_bounds__(kMWarps * 32, CLUSTER || sizeof(T) == 4 ? 3 : kMBlocks)
 cache_decode_masked_kernel(CacheDecode a, DamCacheView c, const unsigned char* __restrict__ blob) {
   dam_chain_prologue();
   using LY = MaskedLayout<D, CLUSTER>;
-  using WS = WarpState<T, D, CODE>;
+  using WS = WarpState<T, D, CODE, PACK>;
   constexpr int kThreads = kMWarps * 32;
   extern __shared__ __align__(128) unsigned char sm[];
   uint32_t* list = reinterpret_cast<uint32_t*>(sm + LY::list_off);
@@ -1127,7 +1146,7 @@ cache_decode_masked_kernel(CacheDecode a, DamCacheView c, const unsigned char* _
 #pragma unroll
       for (int k = 0; k < 2; ++k) {
         const int idx = s * kSlice + Rows<D, 1>::key(row) + 8 * k;
-        if (idx < total) keep |= (list[idx] >> (2 * quad) & 3u) << (2 * k);
+        if (idx < total) keep |= (list[idx] >> WS::head_of(2 * quad) & 3u) << (2 * k);
       }
       const uint32_t slice = ring + it % kMStages * (Rows<D, 1>::bytes + kScales);
       ws.template step<WS::kKeep, 1>(slice, slice + Rows<D, 1>::bytes, keep);
@@ -1173,8 +1192,8 @@ cudaError_t opt_in(int key, int* sm_count) {
   });
 }
 
-// instance number of <T, D, CODE>
-template <typename T, int D, int CODE> constexpr int kInstance = (sizeof(T) == 4) * 4 + (D == 128) * 2 + CODE;
+// instance number of <T, D, CODE, PACK>, one of 12
+template <typename T, int D, int CODE, bool PACK> constexpr int kInstance = (PACK ? 8 : sizeof(T) == 4 ? 4 : 0) + (D == 128) * 2 + CODE;
 
 // Short sequences get a cluster each: of so many blocks that all are resident at once, one per SM (148, 74, 33, 15 and 7 clusters
 // of 1, 2, 4, 8 and 16 blocks: the SMs of a GPC are not a multiple), and no more than have a chunk.  0: there are too many of them.
@@ -1193,14 +1212,14 @@ int64_t short_keys(int split) { return split >= 8 ? 1024 : 2048; }
 // A block each, then, up to 4096 tokens, unless one sequence is longer than an SM's part of all of them.
 constexpr int64_t kManyKeys = 4096;
 
-template <typename T, int D, int CODE, ShortForm FORM>
+template <typename T, int D, int CODE, bool PACK, ShortForm FORM>
 cudaError_t launch_short(const CacheDecode& a, const DamCacheView& c, const CUtensorMap& kmap, const CUtensorMap& vmap, int64_t units, int split,
                          cudaStream_t st) {
   using LY = ShortLayout<D, FORM>;
   if (units * split > 0x7FFFFFFF) return cudaErrorNotSupported;
   int sms = 0;
-  const cudaError_t e = opt_in<cache_decode_short_kernel<T, D, CODE, FORM>, LY::total, FORM == kAlone>(
-      DAM_SETUP_CACHE_SMEM + 24 + 8 * FORM + kInstance<T, D, CODE>, &sms);
+  const cudaError_t e = opt_in<cache_decode_short_kernel<T, D, CODE, PACK, FORM>, LY::total, FORM == kAlone>(
+      DAM_SETUP_CACHE_SMEM + 36 + 12 * FORM + kInstance<T, D, CODE, PACK>, &sms);
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(units * split)); cfg.blockDim = dim3(LY::warps * 32); cfg.dynamicSmemBytes = LY::total; cfg.stream = st;
@@ -1210,15 +1229,15 @@ cudaError_t launch_short(const CacheDecode& a, const DamCacheView& c, const CUte
   attr[1].id = cudaLaunchAttributeClusterDimension;
   attr[1].val.clusterDim.x = (unsigned)split; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr; cfg.numAttrs = FORM == kAlone ? 2 : 1;
-  return cudaLaunchKernelEx(&cfg, cache_decode_short_kernel<T, D, CODE, FORM>, kmap, vmap, a, c);
+  return cudaLaunchKernelEx(&cfg, cache_decode_short_kernel<T, D, CODE, PACK, FORM>, kmap, vmap, a, c);
 }
 
-template <typename T, int D, int CODE>
+template <typename T, int D, int CODE, bool PACK>
 cudaError_t launch_dense(CacheDecode a, const DamCacheView& c, const dam_cache_t* cache, cudaStream_t st) {
   constexpr int WARPS = D == 128 ? 8 : 16, STAGES = D == 128 ? 3 : 2;
   using LY = DenseLayout<D, WARPS, STAGES>;
   int sms = 0;
-  cudaError_t e = opt_in<cache_decode_kernel<T, D, CODE, WARPS, STAGES>, LY::total>(DAM_SETUP_CACHE_SMEM + kInstance<T, D, CODE>, &sms);
+  cudaError_t e = opt_in<cache_decode_kernel<T, D, CODE, PACK, WARPS, STAGES>, LY::total>(DAM_SETUP_CACHE_SMEM + kInstance<T, D, CODE, PACK>, &sms);
   if (e != cudaSuccess) return e;
   const int64_t heads = (int64_t)c.Hkv * a.NS;
   int64_t most = 0, longest = 0;
@@ -1236,10 +1255,10 @@ cudaError_t launch_dense(CacheDecode a, const DamCacheView& c, const dam_cache_t
 
   const int64_t units = heads * c.num_seqs;
   const int split = short_split(units, longest, ShortLayout<D, kAlone>::warps * kKeys);
-  if (split && longest <= split * short_keys(split)) return launch_short<T, D, CODE, kAlone>(a, c, kmap, vmap, units, split, st);
+  if (split && longest <= split * short_keys(split)) return launch_short<T, D, CODE, PACK, kAlone>(a, c, kmap, vmap, units, split, st);
   if (!split && longest <= kManyKeys && longest * blocks <= cache->total_tokens * heads)
-    return units <= 4 * blocks ? launch_short<T, D, CODE, kPairs>(a, c, kmap, vmap, units, 1, st)
-                               : launch_short<T, D, CODE, kFours>(a, c, kmap, vmap, units, 1, st);
+    return units <= 4 * blocks ? launch_short<T, D, CODE, PACK, kPairs>(a, c, kmap, vmap, units, 1, st)
+                               : launch_short<T, D, CODE, PACK, kFours>(a, c, kmap, vmap, units, 1, st);
 
   // all heads side by side where that leaves no more than an eighth of the SMs without work; and no more shares than there can be
   // chunks
@@ -1248,7 +1267,7 @@ cudaError_t launch_dense(CacheDecode a, const DamCacheView& c, const dam_cache_t
   const int64_t list = a.side > 1 ? most : most * heads;
   if (list < shares) shares = list > 0 ? list : 1;
   float* partial = reinterpret_cast<float*>(a.scratch + 64);
-  e = dam_launch_chained(cache_decode_kernel<T, D, CODE, WARPS, STAGES>, dim3((unsigned)(shares * a.side)), dim3(WARPS * 32), LY::total, st, kmap,
+  e = dam_launch_chained(cache_decode_kernel<T, D, CODE, PACK, WARPS, STAGES>, dim3((unsigned)(shares * a.side)), dim3(WARPS * 32), LY::total, st, kmap,
                          vmap, a, c, partial);
   if (e != cudaSuccess || shares == 1 || longest <= LY::chunk) return e;   // (then every sequence is whole in one block)
   const int64_t grid = heads * (a.G < kGMaxGroup ? a.G : kGMaxGroup) * c.num_seqs;
@@ -1256,12 +1275,12 @@ cudaError_t launch_dense(CacheDecode a, const DamCacheView& c, const dam_cache_t
   return dam_launch_chained(cache_join_kernel<T, D>, dim3((unsigned)grid), dim3(256), 0, st, a, c, (const float*)partial, LY::chunk, (int)shares);
 }
 
-template <typename T, int D, int CODE>
+template <typename T, int D, int CODE, bool PACK>
 cudaError_t launch_masked(const CacheDecode& a, const DamCacheView& c, const void* mask, cudaStream_t st) {
   constexpr int kOne = MaskedLayout<D, false>::total, kMany = MaskedLayout<D, true>::total;
   int sms = 0;
-  cudaError_t e = opt_in<cache_decode_masked_kernel<T, D, CODE, false>, kOne>(DAM_SETUP_CACHE_SMEM + 8 + kInstance<T, D, CODE>, &sms);
-  if (e == cudaSuccess) e = opt_in<cache_decode_masked_kernel<T, D, CODE, true>, kMany>(DAM_SETUP_CACHE_SMEM + 16 + kInstance<T, D, CODE>, &sms);
+  cudaError_t e = opt_in<cache_decode_masked_kernel<T, D, CODE, PACK, false>, kOne>(DAM_SETUP_CACHE_SMEM + 12 + kInstance<T, D, CODE, PACK>, &sms);
+  if (e == cudaSuccess) e = opt_in<cache_decode_masked_kernel<T, D, CODE, PACK, true>, kMany>(DAM_SETUP_CACHE_SMEM + 24 + kInstance<T, D, CODE, PACK>, &sms);
   if (e != cudaSuccess) return e;
   const int64_t units = (int64_t)c.num_seqs * c.Hkv * a.NS;
   const int split = masked_split(units);
@@ -1274,14 +1293,16 @@ cudaError_t launch_masked(const CacheDecode& a, const DamCacheView& c, const voi
   attr[1].id = cudaLaunchAttributeClusterDimension;
   attr[1].val.clusterDim.x = (unsigned)split; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr; cfg.numAttrs = split > 1 ? 2 : 1;
-  return cudaLaunchKernelEx(&cfg, split > 1 ? cache_decode_masked_kernel<T, D, CODE, true> : cache_decode_masked_kernel<T, D, CODE, false>, a, c,
+  return cudaLaunchKernelEx(&cfg, split > 1 ? cache_decode_masked_kernel<T, D, CODE, PACK, true> : cache_decode_masked_kernel<T, D, CODE, PACK, false>, a, c,
                             reinterpret_cast<const unsigned char*>(mask));
 }
 
 template <typename T, int D, int CODE>
 cudaError_t launch(const CacheDecode& a, const dam_cache_t* cache, const void* mask, cudaStream_t st) {
   const DamCacheView c = dam_cache_view(cache);
-  return mask ? launch_masked<T, D, CODE>(a, c, mask, st) : launch_dense<T, D, CODE>(a, c, cache, st);
+  if constexpr (sizeof(T) == 4)
+    if (a.G <= kPackGroup) return mask ? launch_masked<T, D, CODE, true>(a, c, mask, st) : launch_dense<T, D, CODE, true>(a, c, cache, st);
+  return mask ? launch_masked<T, D, CODE, false>(a, c, mask, st) : launch_dense<T, D, CODE, false>(a, c, cache, st);
 }
 
 }  // namespace

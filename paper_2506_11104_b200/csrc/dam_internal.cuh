@@ -331,7 +331,7 @@ typedef cudaError_t (*dam_device_setup_fn)(void);
 class DamDeviceTable {
  public:
   static constexpr int kMaxDevices = 64;
-  static constexpr int kMaxSetups = 96;
+  static constexpr int kMaxSetups = 128;
   // The record of `device`, filled by `query` the first time the ordinal is seen.
   cudaError_t info(int device, dam_device_query_fn query, DamDeviceInfo* out);
   // Runs `fn` (with `device` current) unless set-up step `key` already succeeded on that device.
