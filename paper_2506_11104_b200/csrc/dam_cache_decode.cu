@@ -498,7 +498,11 @@ struct CacheDecode {
 // heads), all of them, are served side by side, a block for each in every share: the rows that neighbouring blocks read at about the
 // same time are neighbours in memory.  side == 1: the list goes through the (KV head, group) of each sequence one after the other.
 // Where a share ends inside a sequence's keys it leaves a partial result, and a second kernel joins those.
-constexpr int kMaxShares = 148;        // blocks: one per SM of a B200
+constexpr int kMaxSms = 148;           // of a B200
+// Blocks per SM: the rows on their way fill the shared memory with one of head_dim 128, and half of it with one of 64; there two, whose
+// ends of a sequence fall under one another's work (against one of 16 warps: 6 ragged fp32 sequences of 4 heads 20.7 -> 18.6 us, 64 x
+// 8000 tokens of 8 bf16 heads 86 -> 82, 64 x 16000 143 -> 147; a third stage instead: 19.6 us for the 6).
+template <int D> constexpr int kListBlocks = D == 128 ? 1 : 2;
 
 // (EARLY: of the joining kernel, before it waits for the one before it: past the L1 cache, whose lines may be older than that wait)
 template <bool EARLY = false>
@@ -618,7 +622,7 @@ __device__ __forceinline__ void drain(uint32_t bars, int stages, uint32_t phases
 }
 
 template <typename T, int D, int CODE, bool PACK, int WARPS, int STAGES>
-__global__ void __launch_bounds__(WARPS * 32, 1)
+__global__ void __launch_bounds__(WARPS * 32, kListBlocks<D>)
 cache_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUtensorMap vmap, CacheDecode a, DamCacheView c,
                     float* __restrict__ partial) {
   using LY = DenseLayout<D, WARPS, STAGES>;
@@ -1234,7 +1238,7 @@ cudaError_t launch_short(const CacheDecode& a, const DamCacheView& c, const CUte
 
 template <typename T, int D, int CODE, bool PACK>
 cudaError_t launch_dense(CacheDecode a, const DamCacheView& c, const dam_cache_t* cache, cudaStream_t st) {
-  constexpr int WARPS = D == 128 ? 8 : 16, STAGES = D == 128 ? 3 : 2;
+  constexpr int WARPS = 8, STAGES = D == 128 ? 3 : 2;
   using LY = DenseLayout<D, WARPS, STAGES>;
   int sms = 0;
   cudaError_t e = opt_in<cache_decode_kernel<T, D, CODE, PACK, WARPS, STAGES>, LY::total>(DAM_SETUP_CACHE_SMEM + kInstance<T, D, CODE, PACK>, &sms);
@@ -1251,7 +1255,7 @@ cudaError_t launch_dense(CacheDecode a, const DamCacheView& c, const dam_cache_t
   if (!dam_make_tmap_codes(&kmap, c.k, D, c.Hkv, cache->total_tokens, c.kst, c.ksh, kKeys) ||
       !dam_make_tmap_codes(&vmap, c.v, D, c.Hkv, cache->total_tokens, c.vst, c.vsh, kKeys))
     return cudaErrorInvalidValue;
-  const int blocks = sms < kMaxShares ? sms : kMaxShares;
+  const int blocks = sms < kMaxSms ? sms : kMaxSms;
 
   const int64_t units = heads * c.num_seqs;
   const int split = short_split(units, longest, ShortLayout<D, kAlone>::warps * kKeys);
@@ -1260,10 +1264,11 @@ cudaError_t launch_dense(CacheDecode a, const DamCacheView& c, const dam_cache_t
     return units <= 4 * blocks ? launch_short<T, D, CODE, PACK, kPairs>(a, c, kmap, vmap, units, 1, st)
                                : launch_short<T, D, CODE, PACK, kFours>(a, c, kmap, vmap, units, 1, st);
 
-  // all heads side by side where that leaves no more than an eighth of the SMs without work; and no more shares than there can be
-  // chunks
-  a.side = heads > 1 && heads <= blocks && blocks % heads * 8 <= blocks ? (int)heads : 1;
-  int64_t shares = blocks / a.side;
+  // all heads side by side where that leaves no more than an eighth of the blocks' places without work; and no more shares than
+  // there can be chunks
+  const int places = blocks * kListBlocks<D>;
+  a.side = heads > 1 && heads <= places && places % heads * 8 <= places ? (int)heads : 1;
+  int64_t shares = places / a.side;
   const int64_t list = a.side > 1 ? most : most * heads;
   if (list < shares) shares = list > 0 ? list : 1;
   float* partial = reinterpret_cast<float*>(a.scratch + 64);
@@ -1308,7 +1313,7 @@ cudaError_t launch(const CacheDecode& a, const dam_cache_t* cache, const void* m
 }  // namespace
 
 size_t dam_cache_scratch_bytes(int head_dim) {
-  return 256 + 2ull * kMaxShares * 4 * (head_dim == 128 ? kPartial<128> : kPartial<64>);
+  return 256 + 2ull * kMaxSms * 4 * (head_dim == 128 ? kListBlocks<128> * kPartial<128> : kListBlocks<64> * kPartial<64>);
 }
 
 cudaError_t dam_launch_cache_decode(const void* q, const dam_cache_t* cache, const void* mask, const int32_t* positions, int Hq, int dtype,
