@@ -499,8 +499,8 @@ struct CacheDecode {
 // same time are neighbours in memory.  side == 1: the list goes through the (KV head, group) of each sequence one after the other.
 // Where a share ends inside a sequence's keys it leaves a partial result, and a second kernel joins those.
 constexpr int kMaxSms = 148;           // of a B200
-// Blocks per SM: the rows on their way fill the shared memory with one of head_dim 128, and half of it with one of 64; there two, whose
-// ends of a sequence fall under one another's work (against one of 16 warps: 6 ragged fp32 sequences of 4 heads 20.7 -> 18.6 us, 64 x
+// Blocks per SM: one for head_dim 128 (two of four warps: one sequence of 65000 tokens 25.3 -> 26.6 us, 64 x 32k 549 -> 536), two for 64,
+// where the ends of a sequence fall under the other's work (against one of 16 warps: 6 ragged fp32 sequences of 4 heads 20.7 -> 18.6 us, 64 x
 // 8000 tokens of 8 bf16 heads 86 -> 82, 64 x 16000 143 -> 147; a third stage instead: 19.6 us for the 6).
 template <int D> constexpr int kListBlocks = D == 128 ? 1 : 2;
 
@@ -1238,7 +1238,8 @@ cudaError_t launch_short(const CacheDecode& a, const DamCacheView& c, const CUte
 
 template <typename T, int D, int CODE, bool PACK>
 cudaError_t launch_dense(CacheDecode a, const DamCacheView& c, const dam_cache_t* cache, cudaStream_t st) {
-  constexpr int WARPS = 8, STAGES = D == 128 ? 3 : 2;
+  // (two stages, 128 KB per SM on their way or at work, for either head_dim: a third made 64 x 32k tokens 568 us instead of 549)
+  constexpr int WARPS = 8, STAGES = 2;
   using LY = DenseLayout<D, WARPS, STAGES>;
   int sms = 0;
   cudaError_t e = opt_in<cache_decode_kernel<T, D, CODE, PACK, WARPS, STAGES>, LY::total>(DAM_SETUP_CACHE_SMEM + kInstance<T, D, CODE, PACK>, &sms);
