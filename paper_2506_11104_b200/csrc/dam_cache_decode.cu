@@ -18,7 +18,7 @@
 // registers.
 //
 // Bound by HBM: 2 d bytes and two scales per key and KV head are read once.  64 sequences of 16k to 32k tokens (8 KV heads of 128,
-// int8): 500 to 580 us, 5.8 to 6.6 TB/s of codes and scales; one of 64k to 128k tokens 37 us with its 7 us of beginning and end.
+// int8): 500 to 560 us, 5.8 to 6.6 TB/s of codes and scales; one of 64k to 128k tokens 37 us with its 7 us of beginning and end.
 // A slice costs about 320 warp instructions, a third of them the conversion of its codes (int8: exclusive or, byte permutation and
 // one subtraction for two codes; e4m3: one conversion), and 175 cycles of its SM's share of the bandwidth: with the copies issued
 // by the lanes (cp.async, 600 instructions in all) the same batch took 820 us.
