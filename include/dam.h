@@ -348,6 +348,9 @@ dam_status_t dam_cache_read(const dam_cache_t* cache, const dam_shape_t* tokens,
  * Tokens 0..i must have been written; codes behind them may hold anything, an E4M3 NaN code (0x7F, 0xFF) included, but no
  * written token has one. num_q_heads must be a multiple of the cache's num_kv_heads; softmax_scale 0 selects
  * 1 / sqrt(head_dim). Errors: INVALID_ARGUMENT, UNSUPPORTED (head_dim), BUFFER_TOO_SMALL, CUDA.
+ * Accuracy: logits, softmax and sums are single precision. The weight of a key (its probability times the scale of its V) is
+ * rounded to 11 bits where dtype is BF16, to 22 where it is FP32, and no finer than 2^-36 of the largest weight that the same
+ * query gives a key.
  */
 dam_status_t dam_cache_decode_attention(const void* q, const dam_cache_t* cache, const void* mask, const int32_t* positions_dev,
                                         int32_t num_q_heads, int32_t dtype, float softmax_scale, void* O, float* lse,

@@ -6,10 +6,11 @@
 // scales are applied to the logits and to the probabilities, one multiplication per key and head instead of one per element.
 // Both products are taken transposed, S^T = K q^T and O^T = V^T P^T: the 8 query heads of a KV head are the narrow side of the
 // instruction's tile, so nothing of it is padding where a group has 8 heads.  fp16 operands: q is scaled by a power of two so
-// that its largest element lies in [2^14, 2^15) (a bf16 q is then exact wherever it matters), the probabilities are taken
-// relative to a running maximum times sV over a running reference, at most 2^15.  An fp32 q and its probabilities are each the
-// sum of two fp16 numbers (22 bits), at the price of twice the instructions.  What fp16's last step of 2^-24 drops of a weight is
-// 2^-31 of the largest V a scale can stand for, in either type.
+// that its largest element lies in [2^14, 2^15) (a bf16 q is then exact wherever it matters), and the weights, probability times sV,
+// are held in units of their own for every head: a power of two that puts the largest weight of the head so far between 2^11 and
+// 2^15.  An fp32 q and its weights are each the sum of two fp16 numbers (22 bits), at the price of twice the instructions.  What fp16's
+// last step of 2^-24 drops of a weight is 2^-36 of the head's largest, in either type: a key that the head does not keep, or that has
+// no probability, costs the others nothing however large its V is.
 //
 // A warp works on slices of 16 keys (two at a time where keys are contiguous: two independent chains of instructions), brought to
 // shared memory by asynchronous copies ahead of their use, and keeps a running softmax and its share of O^T of its own; the warps of
@@ -144,13 +145,13 @@ struct WarpState {
   uint32_t qh[KS][2], ql[kSplit ? KS : 1][2];
   float qs[2];                         // logits (log2 units) per product of codes and q as it is held, of the lane's heads
   float m[2], l[2];                    // reference (log2 units) and the lane's share of the sum
-  float vinv;                          // the reference of the V scales: P is held times sV * vinv
+  float unit[2];                       // a weight p sV of the lane's heads is held times this power of two, 2^-116 to 2^120
   float o[KS][4];                      // [u][0..1]: dimension D / 8 * row + 2 u, the lane's heads; [u][2..3]: the next dimension
 
   __device__ __forceinline__ void reset() {
     m[0] = m[1] = -CUDART_INF_F;
     l[0] = l[1] = 0.f;
-    vinv = 1.6225927682921336e32f;     // 2^107
+    unit[0] = unit[1] = 1.329227995784916e36f;               // 2^120: smaller weights than 2^-109 get no larger unit
 #pragma unroll
     for (int u = 0; u < KS; ++u) o[u][0] = o[u][1] = o[u][2] = o[u][3] = 0.f;
   }
@@ -255,8 +256,7 @@ struct WarpState {
         }
       }
     }
-    float x[N][4], c[N][2];
-    bool far = false;
+    float x[N][4];
 #pragma unroll
     for (int n = 0; n < N; ++n) {
 #pragma unroll
@@ -265,14 +265,11 @@ struct WarpState {
         if constexpr (PACK) y += __shfl_xor_sync(0xFFFFFFFFu, y, 2);
         x[n][e] = kept(n, e) ? y * (ks[n][e >> 1] * qs[e & 1]) : -CUDART_INF_F;
       }
-      c[n][0] = vs[n][0] * vinv;
-      c[n][1] = UNIFORM ? c[n][0] : vs[n][1] * vinv;
-      // (one that is not kept does not count; a slice of the first keys may have none)
-      far |= ((ALL || keep[n] & 3u) && c[n][0] > 128.f) || (!UNIFORM && (keep[n] & 12u) && c[n][1] > 128.f);
     }
-    // The reference of the logits moves when one lies more than 8 above it (probabilities stay below 2^8), that of the V scales
-    // when one reaches 128 times it: most steps move nothing.
-    float top[2];
+    // The reference of a head's logits moves when one lies more than 8 above it (probabilities stay below 2^8), its unit when a weight
+    // passes 2^15: most steps move nothing.
+    float top[2], sum[2], w[N][4], most;
+    bool far = false;
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
       top[e] = fmaxf(x[0][e], x[0][2 + e]);
@@ -280,6 +277,25 @@ struct WarpState {
       for (int n = 1; n < N; ++n) top[e] = fmaxf(top[e], fmaxf(x[n][e], x[n][2 + e]));
       far |= top[e] > m[e] + 8.f;
     }
+    // weights over the units, sums, and the largest weight; of no key, or of logits of -inf alone, nothing has a weight
+    auto weigh = [&](float u0, float u1) {
+      const float ref[2] = {m[0] == -CUDART_INF_F ? 0.f : m[0], m[1] == -CUDART_INF_F ? 0.f : m[1]}, u[2] = {u0, u1};
+      most = sum[0] = sum[1] = 0.f;
+#pragma unroll
+      for (int n = 0; n < N; ++n) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float p = g_ex2(x[n][e] - ref[e & 1]);
+          sum[e & 1] += p;
+          // (a key that is not kept may stand in a block without a scale: 0 * NaN is not 0.  p times the scale first: an unused
+          // unit times a large scale is infinite)
+          w[n][e] = kept(n, e) ? p * vs[n][e >> 1] * u[e & 1] : 0.f;
+          most = fmaxf(most, w[n][e]);
+        }
+      }
+    };
+    weigh(unit[0], unit[1]);
+    far |= most > 32768.f;
     if (__any_sync(0xFFFFFFFFu, far)) {
       float f[2];
 #pragma unroll
@@ -293,48 +309,47 @@ struct WarpState {
         m[e] = mn;
         l[e] *= f[e];
       }
-      float vt = 0.f;
+      weigh(1.f, 1.f);
 #pragma unroll
-      for (int n = 0; n < N; ++n) vt = fmaxf(vt, fmaxf(ALL || keep[n] & 3u ? vs[n][0] : 0.f, ALL || keep[n] & 12u ? vs[n][1] : 0.f));
+      for (int e = 0; e < 2; ++e) {
+        // the largest weight of the head so far (2^11 / unit at least was the largest when the unit was chosen) comes to [2^11, 2^12)
+        float mx = 0.f;
 #pragma unroll
-      for (int d = 1; d < 32; d <<= 1) vt = fmaxf(vt, __shfl_xor_sync(0xFFFFFFFFu, vt, d));
-      if (vt * vinv > 128.f) {
-        const int b = max(1, min(234, 260 - (int)(__float_as_uint(vt) >> 23)));   // vt * 2^(b - 127) lies in [64, 128)
-        const float now = __uint_as_float((uint32_t)b << 23), ratio = now / vinv;
-        vinv = now;
-        f[0] *= ratio; f[1] *= ratio;
+        for (int n = 0; n < N; ++n) mx = fmaxf(mx, fmaxf(w[n][e], w[n][2 + e]));
+        mx = fmaxf(mx, __shfl_xor_sync(0xFFFFFFFFu, mx, 4));
+        mx = fmaxf(mx, __shfl_xor_sync(0xFFFFFFFFu, mx, 8));
+        mx = fmaxf(mx, __shfl_xor_sync(0xFFFFFFFFu, mx, 16));
+        const float over = __uint_as_float(0x7F000000u - __float_as_uint(unit[e]));          // 1 / unit
+        mx = fmaxf(mx, f[e] * (2048.f * over));
+        const float now = __uint_as_float((uint32_t)min(265 - (int)(__float_as_uint(mx) >> 23), 247) << 23);
+        f[e] = f[e] * now * over;                            // (at most 1: the unit grows no more than the weights before have shrunk)
+        unit[e] = now;
+      }
 #pragma unroll
-        for (int n = 0; n < N; ++n) { c[n][0] = vs[n][0] * vinv; c[n][1] = vs[n][1] * vinv; }
+      for (int n = 0; n < N; ++n) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) w[n][e] *= unit[e & 1];
       }
 #pragma unroll
       for (int u = 0; u < KS; ++u) { o[u][0] *= f[0]; o[u][1] *= f[1]; o[u][2] *= f[0]; o[u][3] *= f[1]; }
     }
+    l[0] += sum[0];
+    l[1] += sum[1];
     uint32_t pb[N][2], pl[N][2];
-    // (no key yet, or logits of -inf alone: no weight)
-    const float ref[2] = {m[0] == -CUDART_INF_F ? 0.f : m[0], m[1] == -CUDART_INF_F ? 0.f : m[1]};
 #pragma unroll
     for (int n = 0; n < N; ++n) {
-      float w[4];
-#pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        const float p0 = g_ex2(x[n][e] - ref[e]), p1 = g_ex2(x[n][2 + e] - ref[e]);
-        l[e] += p0 + p1;
-        // (a key that is not kept may stand in a block without a scale: 0 * NaN is not 0)
-        w[e] = kept(n, e) ? p0 * c[n][0] : 0.f;
-        w[2 + e] = kept(n, 2 + e) ? p1 * c[n][1] : 0.f;
-      }
       // P^T as operands (k = key, n = head): the transposes of the two 8 x 8 blocks [key][head]
-      uint32_t h0 = pack_half2(w[0], w[1]), h1 = pack_half2(w[2], w[3]);
+      uint32_t h0 = pack_half2(w[n][0], w[n][1]), h1 = pack_half2(w[n][2], w[n][3]);
       if constexpr (PACK) {
         const float2 f0 = __half22float2(*reinterpret_cast<const __half2*>(&h0)), f1 = __half22float2(*reinterpret_cast<const __half2*>(&h1));
-        if (quad >= 2) { h0 = pack_half2(w[0] - f0.x, w[1] - f0.y); h1 = pack_half2(w[2] - f1.x, w[3] - f1.y); }
+        if (quad >= 2) { h0 = pack_half2(w[n][0] - f0.x, w[n][1] - f0.y); h1 = pack_half2(w[n][2] - f1.x, w[n][3] - f1.y); }
       }
       pb[n][0] = movmatrix_trans(h0);
       pb[n][1] = movmatrix_trans(h1);
       if constexpr (kSplit) {
         const float2 f0 = __half22float2(*reinterpret_cast<const __half2*>(&h0)), f1 = __half22float2(*reinterpret_cast<const __half2*>(&h1));
-        pl[n][0] = movmatrix_trans(pack_half2(w[0] - f0.x, w[1] - f0.y));
-        pl[n][1] = movmatrix_trans(pack_half2(w[2] - f1.x, w[3] - f1.y));
+        pl[n][0] = movmatrix_trans(pack_half2(w[n][0] - f0.x, w[n][1] - f0.y));
+        pl[n][1] = movmatrix_trans(pack_half2(w[n][2] - f1.x, w[n][3] - f1.y));
       }
     }
     // O^T += V^T P^T: the lane's rows are 2 quad, 2 quad + 1, 2 quad + 8, 2 quad + 9; their codes of one dimension are brought
@@ -379,9 +394,9 @@ struct WarpState {
   static constexpr int kRow = D + 4;
   __device__ __forceinline__ void store(float* mg) {
     const int lane = threadIdx.x & 31, row = lane >> 2, quad = lane & 3;
-    const float back = 1.f / vinv;
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
+      const float back = __uint_as_float(0x7F000000u - __float_as_uint(unit[e]));            // 1 / unit
       float s = l[e];
       s += __shfl_xor_sync(0xFFFFFFFFu, s, 4);
       s += __shfl_xor_sync(0xFFFFFFFFu, s, 8);

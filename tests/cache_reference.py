@@ -122,3 +122,20 @@ def lse_tolerance(lse, d, S, n):
     """(sums of the probabilities in fp32, lane by lane, then lanes, warps and blocks)"""
     u = 2.0 ** -24
     return (2 * d + 8) * u * S + 2.0 ** -21 + u * (n / 16 + 64) + 4 * u * abs(lse)
+
+
+def weights(q, K, scales, keep, scale):
+    """One query: the largest weight p_j * scales_j of its kept keys (p: probabilities; scales [n]: V's), and the sum of the
+    weights; float64."""
+    x = scale * (K[keep] @ q)
+    p = np.exp(x - x.max())
+    w = p / p.sum() * scales[keep]
+    return float(w.max()), float(w.sum())
+
+
+def tight_tolerance(O, A, S, wmax, code, n, dtype):
+    """As `tolerance`, with what fp16's last step drops counted against the query's own weights: a weight is held in units in
+    which the largest that its warp has seen for this query is 2^11 or more, off by 2^-25 of one, and takes a code of at most 127
+    (int8) or 448 (e4m3).  wmax: the largest weight of all keys, n of them."""
+    top = 127 if code == "int8" else 448
+    return tolerance(O, A, S, 0.0, n, dtype) + n * top * wmax * 2.0 ** -36

@@ -661,3 +661,74 @@ def test_a_long_sequence_captured_and_replayed_at_other_positions():
             assert torch.equal(got[0], eager[0]) and torch.equal(got[1], eager[1])
             if len(inside) == 2:
                 _check(p, q, [x + 1 + step for x in at], *got)
+
+
+def _check_tight(p, q, positions, O, lse, code, keep=None):
+    """As _check, with the tolerance that a query's own weights give."""
+    Hq, d = q.shape[1], q.shape[2]
+    scale, G = 1.0 / math.sqrt(d), Hq // p.Hkv
+    got, got_l, qh = O.cpu().double().numpy(), lse.cpu().double().numpy(), q.cpu().double().numpy()
+    for b, i in enumerate(positions):
+        K, V = p.k[b].values(i + 1), p.v[b].values(i + 1)
+        for h in range(Hq):
+            kept = np.ones(i + 1, bool) if keep is None else keep(b, h, i)
+            want, want_l, A, S, _, n = R.attention(qh[b, h], K[:, h // G], V[:, h // G], kept, scale)
+            rows = p.v[b].scales[np.arange(i + 1) // p.v[b].block, h // G]
+            wmax, _ = R.weights(qh[b, h], K[:, h // G], rows, kept, scale)
+            tol = R.tight_tolerance(want, A, S, wmax, code, n, q.dtype)
+            off = np.abs(got[b, h] - want)
+            assert (off <= tol).all(), (b, h, i, float((off / tol).max()))
+            assert abs(got_l[b, h] - want_l) <= R.lse_tolerance(want_l, d, S, n), (b, h, got_l[b, h], want_l)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("Hq,d,code", [(2, 64, "int8"), (8, 128, "e4m3"), (8, 64, "e4m3"), (4, 128, "int8")])
+@pytest.mark.parametrize("big", [2.0 ** 20, 2.0 ** 40])
+def test_a_large_v_that_another_head_keeps_costs_a_head_nothing(Hq, d, code, dtype, big):
+    """Heads of one group under patterns: the columns of head 0 lie in a block whose V is `big` times the other heads'."""
+    rng = np.random.default_rng(51)
+    p = _filled(rng, [256], 1, d, code, 16, dtype)
+    p.cache.v_scales[0] *= big
+    p.v = R.unpack(p.cache, "v")
+    L = 64
+    P = np.zeros((Hq, L, L), np.float32)
+    for h in range(Hq):
+        for c in (3, 9) if h == 0 else range(17 + h, 40):
+            P[h, c:, c] = 1
+    shape = B.make_shape([0, 256], Hq, 1, d, dtype, DEV)
+    blob, _ = B.dam_build_masks_from_scores(torch.from_numpy(P.reshape(-1)).to(DEV), shape, B.make_rule(L, 0.3, 0.8))
+    masks = [orc.head_mask_from_probs(x, 256, 0.3, 0.8, 0.5, 1e-8) for x in P]
+
+    def keep(b, h, i):
+        return orc.extended_rows(masks[h].M, masks[h].D, masks[h].V, max(i + 1, L), [i])[0, :i + 1].astype(bool)
+    q = torch.from_numpy(rng.standard_normal((1, Hq, d))).float().to(dtype).to(DEV)
+    for i in (200, 60):
+        O, lse, scratch = B.dam_cache_decode_attention(q, p.cache, _ints([i]), blob)
+        assert B.dam_poll_status(scratch) == 0
+        assert not keep(0, 1, i)[:16].any() and keep(0, 0, i).sum() == 2
+        _check_tight(p, q, [i], O, lse, code, keep)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("lengths,Hq,d,code,place", [
+    ([300], 4, 64, "int8", 0), ([300], 8, 128, "e4m3", 5), ([20000], 8, 64, "e4m3", 0), ([20000, 500], 4, 128, "int8", 7),
+    ([200] * 160, 6, 64, "int8", 3), ([600] * 200, 2, 128, "e4m3", 0)])
+def test_a_large_v_of_an_improbable_key_costs_the_others_nothing(lengths, Hq, d, code, place, dtype):
+    """Every key, in every form: the 16 tokens of one block have logits of about -40 and a V of 2^30 times the others'."""
+    rng = np.random.default_rng(53)
+    p = Pair(lengths, 1, d, code, 16, dtype)
+    at = np.concatenate([np.arange(n) // 16 == place for n in lengths])[:, None, None]
+    x, y = rng.standard_normal((sum(lengths), 1, d)) * 0.3, rng.standard_normal((sum(lengths), 1, d))
+    x[:, :, 0] = np.where(at[:, :, 0], -41.0 * math.sqrt(d) / 8, x[:, :, 0])
+    y = np.where(at, y * 2.0 ** 30, y)
+    x, y = (torch.from_numpy(z).float().to(dtype).to(DEV) for z in (x, y))
+    tokens = B.make_shape(_cu(lengths), 1, 1, d, dtype, DEV)
+    assert B.dam_poll_status(B.dam_cache_write(x, y, tokens, p.cache)) == 0
+    p.k, p.v = R.unpack(p.cache, "k"), R.unpack(p.cache, "v")
+    q = rng.standard_normal((len(lengths), Hq, d))
+    q[:, :, 0] = 8
+    q = torch.from_numpy(q).float().to(dtype).to(DEV)
+    positions = [n - 1 for n in lengths]
+    O, lse, scratch = B.dam_cache_decode_attention(q, p.cache, _ints(positions))
+    assert B.dam_poll_status(scratch) == 0
+    _check_tight(p, q, positions, O, lse, code)
