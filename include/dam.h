@@ -349,8 +349,8 @@ dam_status_t dam_cache_read(const dam_cache_t* cache, const dam_shape_t* tokens,
  * written token has one. num_q_heads must be a multiple of the cache's num_kv_heads; softmax_scale 0 selects
  * 1 / sqrt(head_dim). Errors: INVALID_ARGUMENT, UNSUPPORTED (head_dim), BUFFER_TOO_SMALL, CUDA.
  * Accuracy: logits, softmax and sums are single precision. The weight of a key (its probability times the scale of its V) is
- * rounded to 11 bits where dtype is BF16, to 22 where it is FP32, and no finer than 2^-36 of the largest weight that the same
- * query gives a key.
+ * rounded to 11 bits where dtype is BF16 and to 22 where it is F32, but no finer than 2^-36 (F32: 2^-47) of the largest weight
+ * that the same query gives a key.
  */
 dam_status_t dam_cache_decode_attention(const void* q, const dam_cache_t* cache, const void* mask, const int32_t* positions_dev,
                                         int32_t num_q_heads, int32_t dtype, float softmax_scale, void* O, float* lse,

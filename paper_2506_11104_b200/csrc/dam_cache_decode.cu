@@ -9,8 +9,8 @@
 // that its largest element lies in [2^14, 2^15) (a bf16 q is then exact wherever it matters), and the weights, probability times sV,
 // are held in units of their own for every head: a power of two that puts the largest weight of the head so far between 2^11 and
 // 2^15.  An fp32 q and its weights are each the sum of two fp16 numbers (22 bits), at the price of twice the instructions.  What fp16's
-// last step of 2^-24 drops of a weight is 2^-36 of the head's largest, in either type: a key that the head does not keep, or that has
-// no probability, costs the others nothing however large its V is.
+// last step of 2^-24 drops of a weight is 2^-36 of the head's largest, and 2^-47 where there is a second number, which is held 2^11
+// times larger than the first: a key that the head does not keep, or that has no probability, costs the others nothing however large its V is.
 //
 // A warp works on slices of 16 keys (two at a time where keys are contiguous: two independent chains of instructions), brought to
 // shared memory by asynchronous copies ahead of their use, and keeps a running softmax and its share of O^T of its own; the warps of
@@ -101,6 +101,14 @@ __device__ __forceinline__ void mma_f16(float* c, uint32_t a0, uint32_t a1, uint
 __device__ __forceinline__ uint32_t pack_half2(float lo, float hi) {
   const __half2 h = __floats2half2_rn(lo, hi);
   return *reinterpret_cast<const uint32_t*>(&h);
+}
+// The second number of a weight is held kLow times larger (it is at most 2^4, half a step of 2^15), under codes divided by kLow: exact,
+// int8's step of 2^-11 and e4m3's of 2^-20 are fp16 numbers.
+constexpr float kLow = 2048.f;
+__device__ __forceinline__ uint32_t low_codes(uint32_t h) {
+  uint32_t r;
+  asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(h), "r"(0x10001000u));      // (2^-11, twice)
+  return r;
 }
 // four codes in memory order -> two operand registers (codes 0, 1 and codes 2, 3)
 template <int CODE>
@@ -342,14 +350,17 @@ struct WarpState {
       uint32_t h0 = pack_half2(w[n][0], w[n][1]), h1 = pack_half2(w[n][2], w[n][3]);
       if constexpr (PACK) {
         const float2 f0 = __half22float2(*reinterpret_cast<const __half2*>(&h0)), f1 = __half22float2(*reinterpret_cast<const __half2*>(&h1));
-        if (quad >= 2) { h0 = pack_half2(w[n][0] - f0.x, w[n][1] - f0.y); h1 = pack_half2(w[n][2] - f1.x, w[n][3] - f1.y); }
+        if (quad >= 2) {
+          h0 = pack_half2((w[n][0] - f0.x) * kLow, (w[n][1] - f0.y) * kLow);
+          h1 = pack_half2((w[n][2] - f1.x) * kLow, (w[n][3] - f1.y) * kLow);
+        }
       }
       pb[n][0] = movmatrix_trans(h0);
       pb[n][1] = movmatrix_trans(h1);
       if constexpr (kSplit) {
         const float2 f0 = __half22float2(*reinterpret_cast<const __half2*>(&h0)), f1 = __half22float2(*reinterpret_cast<const __half2*>(&h1));
-        pl[n][0] = movmatrix_trans(pack_half2(w[n][0] - f0.x, w[n][1] - f0.y));
-        pl[n][1] = movmatrix_trans(pack_half2(w[n][2] - f1.x, w[n][3] - f1.y));
+        pl[n][0] = movmatrix_trans(pack_half2((w[n][0] - f0.x) * kLow, (w[n][1] - f0.y) * kLow));
+        pl[n][1] = movmatrix_trans(pack_half2((w[n][2] - f1.x) * kLow, (w[n][3] - f1.y) * kLow));
       }
     }
     // O^T += V^T P^T: the lane's rows are 2 quad, 2 quad + 1, 2 quad + 8, 2 quad + 9; their codes of one dimension are brought
@@ -383,7 +394,7 @@ struct WarpState {
           codes_to_half<CODE>(__byte_perm(vw[2][i], vw[3][i], sel), b);
           const int u = 2 * i + k;
           mma_f16(o[u], a[0], a[1], b[0], b[1], pb[n][0], pb[n][1]);
-          if constexpr (kSplit) mma_f16(o[u], a[0], a[1], b[0], b[1], pl[n][0], pl[n][1]);
+          if constexpr (kSplit) mma_f16(o[u], low_codes(a[0]), low_codes(a[1]), low_codes(b[0]), low_codes(b[1]), pl[n][0], pl[n][1]);
         }
       }
     }
@@ -406,6 +417,7 @@ struct WarpState {
       for (int u = 0; u < KS; ++u) {
         float2 y = make_float2(o[u][e] * back, o[u][2 + e] * back);
         if constexpr (PACK) {
+          if (quad >= 2) { y.x *= 1.f / kLow; y.y *= 1.f / kLow; }
           y.x += __shfl_xor_sync(0xFFFFFFFFu, y.x, 2);
           y.y += __shfl_xor_sync(0xFFFFFFFFu, y.y, 2);
         }

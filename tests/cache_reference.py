@@ -136,6 +136,7 @@ def weights(q, K, scales, keep, scale):
 def tight_tolerance(O, A, S, wmax, code, n, dtype):
     """As `tolerance`, with what fp16's last step drops counted against the query's own weights: a weight is held in units in
     which the largest that its warp has seen for this query is 2^11 or more, off by 2^-25 of one, and takes a code of at most 127
-    (int8) or 448 (e4m3).  wmax: the largest weight of all keys, n of them."""
+    (int8) or 448 (e4m3); the second number of an fp32 weight is held 2^11 times larger.  wmax: the largest weight of all keys, n
+    of them."""
     top = 127 if code == "int8" else 448
-    return tolerance(O, A, S, 0.0, n, dtype) + n * top * wmax * 2.0 ** -36
+    return tolerance(O, A, S, 0.0, n, dtype) + n * top * wmax * 2.0 ** (-36 if dtype == torch.bfloat16 else -47)

@@ -732,3 +732,36 @@ def test_a_large_v_of_an_improbable_key_costs_the_others_nothing(lengths, Hq, d,
     O, lse, scratch = B.dam_cache_decode_attention(q, p.cache, _ints(positions))
     assert B.dam_poll_status(scratch) == 0
     _check_tight(p, q, positions, O, lse, code)
+
+
+@pytest.mark.parametrize("lengths,Hq,d,code", [([300], 4, 64, "int8"), ([500], 8, 128, "e4m3"), ([20000], 8, 64, "e4m3"), ([20000, 500], 4, 128, "int8"),
+                                               ([200] * 160, 6, 64, "int8"), ([600] * 200, 2, 128, "e4m3")])
+def test_fp32_weights_far_below_those_of_keys_without_a_value(lengths, Hq, d, code):
+    """Every 16th key has a probability 2^37 times the others' and a V of zero: the output is the others' alone."""
+    rng = np.random.default_rng(55)
+    T = sum(lengths)
+    p = Pair(lengths, 1, d, code, 64, F32)
+    sink = np.concatenate([np.arange(n) % 16 == 0 for n in lengths])[:, None, None]
+    x, y = rng.standard_normal((T, 1, d)) * 0.1, np.where(sink, 0.0, 0.5 + rng.random((T, 1, d)))
+    x[:, :, 0] = np.where(sink[:, :, 0], 37 * math.log(2) * math.sqrt(d) / 8, 0)
+    x, y = (torch.from_numpy(z).float().to(DEV) for z in (x, y))
+    tokens = B.make_shape(_cu(lengths), 1, 1, d, F32, DEV)
+    assert B.dam_poll_status(B.dam_cache_write(x, y, tokens, p.cache)) == 0
+    p.k, p.v = R.unpack(p.cache, "k"), R.unpack(p.cache, "v")
+    q = rng.standard_normal((len(lengths), Hq, d)) * 0.1
+    q[:, :, 0] = 8
+    q = torch.from_numpy(q).float().to(DEV)
+    positions = [n - 1 for n in lengths]
+    O, lse, scratch = B.dam_cache_decode_attention(q, p.cache, _ints(positions))
+    assert B.dam_poll_status(scratch) == 0
+    _check_tight(p, q, positions, O, lse, code)
+    # and under patterns: the last 48 keys
+    L = 64
+    P = np.tril(np.ones((L, L), np.float32)) - np.tril(np.ones((L, L), np.float32), -48)
+    hm = orc.head_mask_from_probs(P, 200, 0.3, 0.8, 0.5, 1e-8)
+    shape = B.make_shape([200 * k for k in range(len(lengths) + 1)], Hq, 1, d, F32, DEV)
+    maps = torch.from_numpy(np.tile(P.reshape(-1), len(lengths) * Hq)).to(DEV)
+    blob, _ = B.dam_build_masks_from_scores(maps, shape, B.make_rule(L, 0.3, 0.8))
+    O, lse, scratch = B.dam_cache_decode_attention(q, p.cache, _ints(positions), blob)
+    assert B.dam_poll_status(scratch) == 0
+    _check_tight(p, q, positions, O, lse, code, lambda b, h, i: orc.extended_rows(hm.M, hm.D, hm.V, i + 1, [i])[0, :i + 1].astype(bool))
