@@ -127,14 +127,14 @@ struct Coder {
         differ |= __float_as_uint(t[k + 1]) ^ __float_as_uint(b);
       }
       if (differ) {                      // (of bf16 values: one that is an exact tie, or amax / 2)
-        // x - q s is s / 2 there, or next to it, and the difference is exact: a multiple of half an ulp of s
-        const float half = 0.5f * s;
+        // x - q s is s / 2 there, or next to it, and the difference is exact: a multiple of half an ulp of s.  Twice the difference
+        // is compared with s: half of an s below 2^-125 may be no fp32 number.
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
-          const float q = t[k] - kMagic, r = fmaf(-q, s, x[k]);
+          const float q = t[k] - kMagic, twice = 2.f * fmaf(-q, s, x[k]);
           const bool odd = (__float_as_uint(t[k]) & 1u) != 0;
-          if (r > half || (r == half && odd)) t[k] += 1.f;
-          else if (r < -half || (r == -half && odd)) t[k] -= 1.f;
+          if (twice > s || (twice == s && odd)) t[k] += 1.f;
+          else if (twice < -s || (twice == -s && odd)) t[k] -= 1.f;
         }
       }
 #pragma unroll

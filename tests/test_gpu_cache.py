@@ -765,3 +765,28 @@ def test_fp32_weights_far_below_those_of_keys_without_a_value(lengths, Hq, d, co
     O, lse, scratch = B.dam_cache_decode_attention(q, p.cache, _ints(positions), blob)
     assert B.dam_poll_status(scratch) == 0
     _check_tight(p, q, positions, O, lse, code, lambda b, h, i: orc.extended_rows(hm.M, hm.D, hm.V, i + 1, [i])[0, :i + 1].astype(bool))
+
+
+def test_borders_of_codes_under_the_smallest_scales():
+    """int8 scales just above 2^-126: half of one with an odd last bit is no fp32 number."""
+    unit = 2.0 ** -149
+    for s in (2 ** 23 + 1, 2 ** 23 + 77, 2 ** 24 - 1, 2 ** 24 - 3):
+        amax = float(np.float32(s * 127.0 * unit))
+        assert R.scale_of(amax, "int8") == s * unit
+        x = np.zeros((32, 1, 64))
+        for k in range(100):                                  # the fp32 numbers on either side of the border above k, and of the one below -k
+            border = (k + 0.5) * s * unit
+            near = np.float32(border)
+            around = [np.nextafter(near, np.float32(0)), near, np.nextafter(near, np.float32(1))]
+            x.reshape(-1)[10 * k:10 * k + 6] = [float(a) for a in around] + [-float(a) for a in around]
+        x[16:] = x[:16]
+        x[0, 0, 63] = x[16, 0, 63] = amax
+        rows = torch.from_numpy(x).to(torch.float32)
+        assert np.array_equal(rows.double().numpy(), x)
+        p = Pair([64], 1, 64, "int8", 16, F32)
+        p.write(rows.to(DEV), rows.flip(2).contiguous().to(DEV), [32], [0])
+        p.check()
+        for i in range(16):                                   # and one by one: the first row has the scale, the others join it
+            one = rows[i:i + 1].to(DEV)
+            p.write(one, one, [1], [32 + i])
+        p.check()
