@@ -133,13 +133,20 @@ def _stream(device) -> int:
     return _raw_stream(index)
 
 
+# the same for the index of a CUDA device
+_index_stream = _raw_stream if _raw_stream is not None else lambda index: torch.cuda.current_stream(index).cuda_stream
+
+
 class _ByReference:
-    """`ref` is the reference to the structure `c`, made when c is set (every call passes it; byref takes as long as a check)."""
+    """`ref` is the reference to the structure `c`, made when c is set (every call passes it; byref takes as long as a check);
+    `index`: the CUDA device that cu_dev is on, -1 for none."""
 
     def __setattr__(self, name, value):
         object.__setattr__(self, name, value)
         if name == "c":
             object.__setattr__(self, "ref", ctypes.byref(value))
+        elif name == "cu_dev":
+            object.__setattr__(self, "index", -1 if value is None else value.get_device())
 
 
 @dataclass
@@ -149,6 +156,19 @@ class Shape(_ByReference):
     cu_host: np.ndarray
     cu_dev: Optional[torch.Tensor]
     lengths: List[int]
+    kv = None                    # what the K and V rows look like to torch, see _kv_rows
+
+    def __setattr__(self, name, value):
+        super().__setattr__(name, value)
+        if name == "c":
+            self.kv = _kv_rows(value)
+
+
+def _kv_rows(s: dam_shape_t):
+    """(shape of the K and V rows, strides of K, of V, dtype)"""
+    rows = (s.total_tokens, s.num_kv_heads, s.head_dim)
+    return (rows, (s.k_stride_tok, s.k_stride_head, 1), (s.v_stride_tok, s.v_stride_head, 1),
+            torch.bfloat16 if s.dtype == DAM_BF16 else torch.float32)
 
 
 def make_shape(cu_seqlens: Sequence[int], Hq: int, Hkv: int, d: int, dtype: torch.dtype, device=None,
@@ -377,7 +397,8 @@ def make_cache(cu_seqlens: Sequence[int], Hkv: int, d: int, code: str = "int8", 
     """A KV cache held in 8 bits, with room for cu_seqlens[b + 1] - cu_seqlens[b] tokens of sequence b.
 
     Buffers that are not given are allocated on `device` (zeros); codes [tokens, Hkv, d] of one byte, any strides with the
-    last dimension contiguous; scales fp32 [rows, Hkv], contiguous.  Without a device: a description for host-only calls."""
+    last dimension contiguous; scales fp32 [rows, Hkv], contiguous; all on `device`.  Without a device: a description for
+    host-only calls."""
     cu_host = np.ascontiguousarray(cu_seqlens, dtype=np.int32)
     lengths = [int(b - a) for a, b in zip(cu_host[:-1], cu_host[1:])]
     T, (number, dtype) = int(cu_host[-1]), CACHE_CODES[code]
@@ -400,6 +421,9 @@ def make_cache(cu_seqlens: Sequence[int], Hkv: int, d: int, code: str = "int8", 
             assert x.element_size() == 1 and x.shape == (T, Hkv, d) and (x.stride(2) == 1 or x.numel() == 0)
         for x in scales:
             assert x.dtype == torch.float32 and x.is_contiguous() and x.numel() >= rows * Hkv
+        for x in codes + scales:
+            if x.device != cu_dev.device:
+                raise ValueError(f"the cache's buffers belong on the device {cu_dev.device}: got a tensor of {x.device}")
         (c.k_codes, c.v_codes), (c.k_scales, c.v_scales) = map(_ptr, codes), map(_ptr, scales)
     (c.k_stride_tok, c.k_stride_head), (c.v_stride_tok, c.v_stride_head) = (
         (Hkv * d, d) if x is None or x.numel() == 0 else (x.stride(0), x.stride(1)) for x in codes)
@@ -414,22 +438,58 @@ def dam_cache_sizes(cache: Cache, Hq: int):
 
 
 def _per_sequence(x: torch.Tensor, n: int) -> int:
-    """Pointer of an int32 tensor on the device with one element per sequence."""
+    """Pointer of an int32 tensor with one element per sequence."""
     assert x.dtype is torch.int32 and x.numel() == n and x.is_contiguous()
-    if not x.is_cuda:
-        raise ValueError("one number per sequence, on the device: got a tensor of " + str(x.device))
     return x.data_ptr()
+
+
+def _check_device(index: int, **tensors):
+    """ValueError unless all of them (None: not there) are on the CUDA device; Shape and Cache stand for their cu_seqlens."""
+    for name, x in tensors.items():
+        where = index if x is None else x.index if isinstance(x, _ByReference) else x.get_device()
+        if index < 0 or where != index:
+            of = f", which is on {x.device}" if isinstance(x, torch.Tensor) else ", which was made for another"
+            raise ValueError(f"every tensor of a call belongs on the device it runs on: not so {name}{of}")
+
+
+def _check_rows(tokens: "Shape", K: torch.Tensor, V: torch.Tensor):
+    """ValueError unless the rows that `tokens` describes lie inside K and V where K and V have them: K, V [tokens, heads,
+    head_dim] or longer, or [heads, tokens, head_dim], with the strides of `tokens`; or flattened in another way (their last
+    element is no further than K's and V's own).  The calls compare the usual case, the very shape, by themselves."""
+    tokens.kv = rows, *strides, dtype = _kv_rows(tokens.c)
+    T, H, d = rows
+    for name, x, (st, sh, _) in zip("KV", (K, V), strides):
+        if T == 0:
+            continue
+        if x.dtype is not dtype:
+            raise ValueError(f"{name} is of {x.dtype}, its rows are described as {dtype}")
+        # (the stride of a dimension that one element is taken from says nothing)
+        ok = x.dim() == 3 and any(all(x.shape[k] >= n and (n == 1 or x.stride(k) == w) for k, n, w in zip(order, rows, (st, sh, 1)))
+                                  for order in ((0, 1, 2), (1, 0, 2)))
+        if x.dim() != 3 or (not ok and x.is_contiguous() and (H == 1 or x.shape[2] != d)):
+            last = sum((n - 1) * w for n, w in zip(x.shape, x.stride())) if x.numel() else -1
+            ok = (T - 1) * st + (H - 1) * sh + d - 1 <= last
+        if not ok:
+            raise ValueError(f"{name} of shape {tuple(x.shape)} and strides {x.stride()} does not have the rows that `tokens` "
+                             f"describes: {rows}, strides {(st, sh, 1)}")
 
 
 def dam_cache_write(K: torch.Tensor, V: torch.Tensor, tokens: Shape, cache: Cache, starts: Optional[torch.Tensor] = None,
                     scratch: Optional[torch.Tensor] = None) -> torch.Tensor:
     """Quantises the packed rows K, V (`tokens` says how many each sequence gets) into the cache, from token starts[b] of
-    sequence b on (int32 on the device; None: token 0).  Returns scratch."""
-    device = K.device
+    sequence b on (int32 on the device; None: token 0).  Returns scratch.  ValueError for K or V that are not what `tokens`
+    describes, and for a tensor on another device than K."""
+    at = None if starts is None else _per_sequence(starts, cache.num_seqs)
+    index = K.get_device()
     if scratch is None:
-        scratch = _alloc(256, device)
-    rc = lib().dam_cache_write(K.data_ptr(), V.data_ptr(), tokens.ref, None if starts is None else _per_sequence(starts, cache.num_seqs),
-                               cache.ref, scratch.data_ptr(), scratch.numel(), _stream(device))
+        scratch = _alloc(256, K.device)
+    rows, ks, vs, dtype = tokens.kv
+    if not (K.shape == rows and V.shape == rows and K.stride() == ks and V.stride() == vs and K.dtype is dtype and V.dtype is dtype):
+        _check_rows(tokens, K, V)
+    if not (V.get_device() == index == scratch.get_device() and tokens.index == index == cache.index >= 0
+            and (at is None or starts.get_device() == index)):
+        _check_device(index, K=K, V=V, scratch=scratch, tokens=tokens, cache=cache, starts=starts)
+    rc = lib().dam_cache_write(K.data_ptr(), V.data_ptr(), tokens.ref, at, cache.ref, scratch.data_ptr(), scratch.numel(), _index_stream(index))
     if rc:
         _check(rc, "dam_cache_write")
     return scratch
@@ -438,40 +498,60 @@ def dam_cache_write(K: torch.Tensor, V: torch.Tensor, tokens: Shape, cache: Cach
 def dam_cache_read(cache: Cache, tokens: Shape, starts: Optional[torch.Tensor] = None, K: Optional[torch.Tensor] = None,
                    V: Optional[torch.Tensor] = None, scratch: Optional[torch.Tensor] = None):
     """Reads tokens starts[b] ... of every sequence back, as packed rows (`tokens` says how many, of which type and strides).
-    Returns (K, V, scratch)."""
-    device = cache.k_codes.device
-    if K is None or V is None:
-        s = tokens.c
-        rows = [torch.empty_strided((s.total_tokens, s.num_kv_heads, s.head_dim), (*strides, 1), device=device,
-                                    dtype=torch.bfloat16 if s.dtype == DAM_BF16 else torch.float32)
-                for strides in ((s.k_stride_tok, s.k_stride_head), (s.v_stride_tok, s.v_stride_head))]
-        K, V = K if K is not None else rows[0], V if V is not None else rows[1]
+    Returns (K, V, scratch).  ValueError for K or V that are not what `tokens` describes, and for a tensor on another device
+    than the cache."""
+    at = None if starts is None else _per_sequence(starts, cache.num_seqs)
+    index = cache.index
     if scratch is None:
-        scratch = _alloc(256, device)
-    rc = lib().dam_cache_read(cache.ref, tokens.ref, None if starts is None else _per_sequence(starts, cache.num_seqs), K.data_ptr(),
-                              V.data_ptr(), scratch.data_ptr(), scratch.numel(), _stream(device))
+        scratch = _alloc(256, cache.cu_dev.device)
+    if K is None or V is None:
+        shape, ks, vs, dtype = _kv_rows(tokens.c)
+        rows = [torch.empty_strided(shape, strides, device=cache.cu_dev.device, dtype=dtype) for strides in (ks, vs)]
+        K, V = K if K is not None else rows[0], V if V is not None else rows[1]
+    rows, ks, vs, dtype = tokens.kv
+    if not (K.shape == rows and V.shape == rows and K.stride() == ks and V.stride() == vs and K.dtype is dtype and V.dtype is dtype):
+        _check_rows(tokens, K, V)
+    if not (K.get_device() == V.get_device() == index == scratch.get_device() and tokens.index == index >= 0
+            and (at is None or starts.get_device() == index)):
+        _check_device(index, K=K, V=V, scratch=scratch, tokens=tokens, starts=starts)
+    rc = lib().dam_cache_read(cache.ref, tokens.ref, at, K.data_ptr(), V.data_ptr(), scratch.data_ptr(), scratch.numel(), _index_stream(index))
     if rc:
         _check(rc, "dam_cache_read")
     return K, V, scratch
+
+
+def _check_result(x: torch.Tensor, name: str, numel: int, dtype: torch.dtype):
+    if x.dtype is not dtype or not x.is_contiguous() or x.numel() < numel:
+        raise ValueError(f"{name} takes {numel} contiguous elements of {dtype}: got {tuple(x.shape)} of {x.dtype}, strides {x.stride()}")
 
 
 def dam_cache_decode_attention(q: torch.Tensor, cache: Cache, positions: torch.Tensor, mask: Optional[torch.Tensor] = None,
                                softmax_scale: float = 0.0, O: Optional[torch.Tensor] = None,
                                lse: Optional[torch.Tensor] = None, scratch: Optional[torch.Tensor] = None):
     """One new token per sequence against an 8-bit cache (q, O: [B, Hq, d]; positions int32 [B]): every key up to its position,
-    or, with a mask blob, those that its patterns keep.  Returns (O, LSE [B, Hq] fp32, scratch)."""
-    n, Hq, _ = shape = q.shape
-    dtype, device = q.dtype, q.device
+    or, with a mask blob, those that its patterns keep.  Returns (O, LSE [B, Hq] fp32, scratch).  ValueError for an O or lse
+    that cannot take the result, and for a tensor on another device than q."""
+    n, Hq, d = shape = q.shape
+    dtype = q.dtype
     assert shape == (cache.num_seqs, Hq, cache.head_dim) and q.is_contiguous() and (dtype is torch.bfloat16 or dtype is torch.float32)
+    at = _per_sequence(positions, n)
+    index = q.get_device()
+    if scratch is None:
+        scratch = _alloc(dam_cache_sizes(cache, Hq)[1], q.device)
     if O is None:
         O = torch.empty_like(q)
     if lse is None:
-        lse = torch.empty(n, Hq, dtype=torch.float32, device=device)
-    if scratch is None:
-        scratch = _alloc(dam_cache_sizes(cache, Hq)[1], device)
-    rc = lib().dam_cache_decode_attention(q.data_ptr(), cache.ref, None if mask is None else mask.data_ptr(), _per_sequence(positions, n), Hq,
+        lse = torch.empty(n, Hq, dtype=torch.float32, device=q.device)
+    if not (O.get_device() == lse.get_device() == index == scratch.get_device() and positions.get_device() == index == cache.index >= 0
+            and (mask is None or mask.get_device() == index)):
+        _check_device(index, q=q, O=O, lse=lse, scratch=scratch, positions=positions, cache=cache, mask=mask)
+    if not (O.dtype is dtype and O.is_contiguous() and O.numel() == n * Hq * d):
+        _check_result(O, "O", n * Hq * d, dtype)
+    if not (lse.dtype is torch.float32 and lse.is_contiguous() and lse.numel() == n * Hq):
+        _check_result(lse, "lse", n * Hq, torch.float32)
+    rc = lib().dam_cache_decode_attention(q.data_ptr(), cache.ref, None if mask is None else mask.data_ptr(), at, Hq,
                                           DAM_BF16 if dtype is torch.bfloat16 else DAM_F32, softmax_scale, O.data_ptr(), lse.data_ptr(),
-                                          scratch.data_ptr(), scratch.numel(), _stream(device))
+                                          scratch.data_ptr(), scratch.numel(), _index_stream(index))
     if rc:
         _check(rc, "dam_cache_decode_attention")
     return O, lse, scratch

@@ -193,3 +193,85 @@ def test_the_restatement_on_known_blocks():
     y = np.concatenate([np.linspace(-448, 448, 20001), 2.0 ** np.arange(-12, 9), 1.5 * 2.0 ** np.arange(-12, 8.0)]).astype(np.float32)
     want = torch.from_numpy(y).to(torch.float8_e4m3fn).double().numpy()
     assert np.array_equal(R.codes_of(y.astype(np.float64), 1.0, "e4m3"), want)
+
+
+def _rows_call(call, K, V, tokens, cache):
+    buf = torch.zeros(256, dtype=torch.uint8)
+    return B.dam_cache_write(K, V, tokens, cache, None, buf) if call == "write" else B.dam_cache_read(cache, tokens, None, K, V, buf)
+
+
+@pytest.mark.parametrize("call", ["write", "read"])
+def test_rows_that_tokens_does_not_describe_are_refused(call):
+    cache = B.make_cache([0, 64], 4, 64, "e4m3", 16, "cpu")
+    tokens = B.make_shape([0, 40], 8, 4, 64, torch.bfloat16, "cpu")
+    good = torch.zeros(40, 4, 64, dtype=torch.bfloat16)
+    fused = torch.zeros(40, 16, 64, dtype=torch.bfloat16)
+    for bad in (fused[:, 8:12], fused, good.float(), good[:39], good[:, :3], good[:, :, :32], good.half(), good[::2],
+                good.permute(1, 0, 2).contiguous(), good.reshape(-1)[:-1], good.reshape(40, 256)[:, :128], good.reshape(40, 256)[:39]):
+        for K, V in ((bad, good), (good, bad)):
+            with pytest.raises(ValueError, match="rows"):
+                _rows_call(call, K, V, tokens, cache)
+    # described with the strides of a fused tensor, but not one
+    wide = B.make_shape([0, 40], 8, 4, 64, torch.bfloat16, "cpu", k_strides=(1024, 64), v_strides=(1024, 64))
+    for bad in (good, good.reshape(40, 256), good.reshape(-1)):
+        with pytest.raises(ValueError, match="rows"):
+            _rows_call(call, bad, fused[:, 8:12], wide, cache)
+
+
+@pytest.mark.parametrize("call", ["write", "read"])
+def test_rows_described_in_every_way_are_taken(call):
+    """(What is wrong here is that the tensors are not on a GPU.)"""
+    cache = B.make_cache([0, 64], 4, 64, "e4m3", 16, "cpu")
+    plain = torch.zeros(40, 4, 64, dtype=torch.bfloat16)
+    fused, longer = torch.zeros(48, 16, 64, dtype=torch.bfloat16), torch.zeros(64, 4, 64, dtype=torch.bfloat16)
+    major = torch.zeros(4, 64, 64, dtype=torch.bfloat16)
+
+    def ok(x, strides=None, n=40, tokens=None):
+        tokens = tokens or B.make_shape([0, n], 8, 4, 64, torch.bfloat16, "cpu", k_strides=strides, v_strides=strides)
+        with pytest.raises(ValueError, match="on the device"):
+            _rows_call(call, x, x, tokens, cache)
+        return tokens
+
+    ok(plain), ok(longer), ok(plain.reshape(40, 256)), ok(plain.reshape(-1)), ok(longer.reshape(1, 64, 4, 64)), ok(longer.reshape(2, 32, 256))
+    ok(fused[:, 8:12], (1024, 64)), ok(fused, (1024, 64)), ok(fused.reshape(48, 1024)[:, 256:], (1024, 64)), ok(fused[4:44, ::4], (1024, 256))
+    ok(major.permute(1, 0, 2), (64, 4096)), ok(major, (64, 4096)), ok(major[:, 3:43], (64, 4096))
+    ok(plain.as_strided((1, 4, 64), (8, 64, 1)), n=1), ok(torch.zeros(0, 4, 64, dtype=torch.bfloat16), n=0), ok(plain.float(), n=0), ok(major, n=0)
+    # the description may change
+    tokens = ok(plain)
+    tokens.c.k_stride_tok = tokens.c.v_stride_tok = 1024
+    ok(fused[:, 8:12], tokens=tokens), ok(fused[:, :4], tokens=tokens)
+    tokens.c = B.make_shape([0, 40], 8, 4, 64, torch.float32, "cpu").c
+    ok(plain.float(), tokens=tokens)
+    one = B.make_cache([0, 64], 1, 64, "e4m3", 16, "cpu")
+    batch = torch.zeros(2, 20, 64, dtype=torch.bfloat16)
+    with pytest.raises(ValueError, match="on the device"):
+        _rows_call(call, batch, batch, B.make_shape([0, 40], 8, 1, 64, torch.bfloat16, "cpu"), one)
+
+
+def test_results_that_cannot_be_written_are_refused(monkeypatch):
+    cache = B.make_cache([0, 64, 128], 1, 64, "e4m3", 16, "cpu")
+    buf, i = torch.zeros(1 << 22, dtype=torch.uint8), torch.zeros(2, dtype=torch.int32)
+    for dtype in (torch.bfloat16, torch.float32):
+        q, other = torch.zeros(2, 4, 64, dtype=dtype), torch.float32 if dtype is torch.bfloat16 else torch.bfloat16
+        lse = torch.zeros(2, 4)
+        for O in (q.to(other), torch.zeros(2, 8, 64, dtype=dtype)[:, ::2], torch.zeros(1, 4, 64, dtype=dtype), torch.zeros(64, 4, 2, dtype=dtype).permute(2, 1, 0)):
+            with monkeypatch.context() as m, pytest.raises(ValueError, match="O takes"):
+                m.setattr(B, "_check_device", lambda *args, **tensors: None)
+                B.dam_cache_decode_attention(q, cache, i, None, 0.0, O, lse, buf)
+        for bad in (lse.double(), lse.bfloat16(), torch.zeros(4, 2).t(), torch.zeros(7)):
+            with monkeypatch.context() as m, pytest.raises(ValueError, match="lse takes"):
+                m.setattr(B, "_check_device", lambda *args, **tensors: None)
+                B.dam_cache_decode_attention(q, cache, i, None, 0.0, q.clone(), bad, buf)
+        for O, l in ((q.clone(), lse), (torch.zeros(3, 4, 64, dtype=dtype), torch.zeros(9))):
+            B._check_result(O, "O", q.numel(), dtype)
+            B._check_result(l, "lse", 8, torch.float32)
+            with pytest.raises(ValueError, match="on the device"):
+                B.dam_cache_decode_attention(q, cache, i, None, 0.0, O, l, buf)
+
+
+def test_a_cache_s_buffers_belong_on_its_device():
+    codes = torch.zeros(64, 1, 64, dtype=torch.int8, device="meta")
+    scales = torch.zeros(5, 1, device="meta")
+    for given in ({"k_codes": codes}, {"v_codes": codes}, {"k_scales": scales}, {"v_scales": scales}):
+        with pytest.raises(ValueError, match="on the device"):
+            B.make_cache([0, 64], 1, 64, "int8", 16, "cpu", **given)

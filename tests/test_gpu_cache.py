@@ -790,3 +790,33 @@ def test_borders_of_codes_under_the_smallest_scales():
             one = rows[i:i + 1].to(DEV)
             p.write(one, one, [1], [32 + i])
         p.check()
+
+
+def test_tensors_in_host_memory_are_refused_whichever_they_are():
+    """Before anything is launched."""
+    rng = np.random.default_rng(57)
+    p = _filled(rng, [256], 1, 64, "int8", 64, BF16)
+    blob, _ = _blob(rng, [256], 2, 64)
+    tokens, hosted = B.make_shape([0, 30], 1, 1, 64, BF16, DEV), B.make_shape([0, 30], 1, 1, 64, BF16)
+    x = _rows(rng, 30, 1, 64, BF16)
+    start, small = _ints([0]), torch.empty(256, dtype=torch.uint8, device=DEV)
+    args = {"K": x, "V": x.clone(), "tokens": tokens, "starts": start, "scratch": small}
+    for name in args:
+        bad = dict(args)
+        bad[name] = hosted if name == "tokens" else args[name].cpu()
+        with pytest.raises(ValueError, match="on the device"):
+            B.dam_cache_write(bad["K"], bad["V"], bad["tokens"], p.cache, bad["starts"], bad["scratch"])
+        with pytest.raises(ValueError, match="on the device"):
+            B.dam_cache_read(p.cache, bad["tokens"], bad["starts"], bad["K"], bad["V"], bad["scratch"])
+    q = torch.ones(1, 2, 64, dtype=BF16, device=DEV)
+    scratch = torch.empty(B.dam_cache_sizes(p.cache, 2)[1], dtype=torch.uint8, device=DEV)
+    args = {"q": q, "positions": _ints([99]), "mask": blob, "O": torch.zeros_like(q), "lse": torch.zeros(1, 2, device=DEV), "scratch": scratch}
+    for name in args:
+        bad = dict(args)
+        bad[name] = args[name].cpu()
+        with pytest.raises(ValueError, match="on the device"):
+            B.dam_cache_decode_attention(bad["q"], p.cache, bad["positions"], bad["mask"], 0.0, bad["O"], bad["lse"], bad["scratch"])
+    p.check()
+    assert not args["O"].any()
+    B.dam_cache_decode_attention(**args, cache=p.cache)
+    assert args["O"].any()
