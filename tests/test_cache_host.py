@@ -275,3 +275,13 @@ def test_a_cache_s_buffers_belong_on_its_device():
     for given in ({"k_codes": codes}, {"v_codes": codes}, {"k_scales": scales}, {"v_scales": scales}):
         with pytest.raises(ValueError, match="on the device"):
             B.make_cache([0, 64], 1, 64, "int8", 16, "cpu", **given)
+
+
+def test_the_restatement_rounds_to_the_code_it_should():
+    """Quotients that are exact and no ties, under scales of 1 and 2^-6."""
+    s = R.Side(16, 1, 4, "int8", 16)
+    s.write(np.array([[[127.0, -50.25, 0.0, 63.75]]]), 0)    # scale 1
+    assert s.scales[0, 0] == 1 and s.codes[0, 0].tolist() == [127, -50, 0, 64]
+    s = R.Side(16, 1, 4, "int8", 16)
+    s.write(np.array([[[127.0, -50.25, 0.0, 63.75]]]) / 64, 0)
+    assert s.scales[0, 0] == 2.0 ** -6 and s.codes[0, 0].tolist() == [127, -50, 0, 64]

@@ -820,3 +820,48 @@ def test_tensors_in_host_memory_are_refused_whichever_they_are():
     assert not args["O"].any()
     B.dam_cache_decode_attention(**args, cache=p.cache)
     assert args["O"].any()
+
+
+@pytest.mark.parametrize("Hkv,d,dtype,code,block", [(2, d, dtype, code, block) for d in (64, 128) for dtype in (BF16, F32) for code in ("int8", "e4m3")
+                                                    for block in (16, 32, 64, 128) if (d, dtype, code, block) not in {f[1:] for f in FORMS}])
+def test_write_and_read_bit_for_bit_in_every_other_form(Hkv, d, dtype, code, block):
+    test_write_and_read_bit_for_bit(Hkv, d, dtype, code, block)
+
+
+# fp32 queries of few heads (two numbers in one tile) and of many, in the list, in clusters and in a block each
+FP32 = [([9000, 17000, 3], 8, 2, 64, "e4m3", 16), ([20000, 500], 8, 1, 64, "int8", 64), ([20000, 500], 8, 1, 128, "e4m3", 64), ([18000], 2, 1, 128, "int8", 128),
+        ([1500, 40], 8, 1, 64, "int8", 64), ([1500, 40], 8, 1, 128, "e4m3", 32), ([33, 128, 190] * 100, 5, 1, 128, "int8", 64),
+        ([40, 250, 129, 64, 1] * 40, 16, 4, 128, "e4m3", 32), ([300, 700] * 100, 6, 1, 64, "e4m3", 16), ([1000] * 160, 2, 1, 64, "int8", 64)]
+
+
+@pytest.mark.parametrize("lengths,Hq,Hkv,d,code,block", FP32)
+def test_attention_of_fp32_queries_however_the_keys_are_shared(lengths, Hq, Hkv, d, code, block):
+    test_attention_however_the_keys_are_shared(lengths, Hq, Hkv, d, F32, code, block)
+
+
+@pytest.mark.parametrize("lengths,Hq,Hkv,d,code,block,pcl", [
+    ([700, 400], 8, 2, 128, "int8", 64, 128), ([700, 130, 1], 4, 4, 64, "e4m3", 16, 100), ([300, 500], 4, 1, 64, "int8", 128, 96),
+    ([200] * 90, 9, 3, 128, "e4m3", 32, 64), ([200] * 120, 6, 2, 64, "int8", 16, 64), ([200] * 240, 5, 1, 128, "int8", 64, 64)])
+def test_attention_of_fp32_queries_under_stored_patterns(lengths, Hq, Hkv, d, code, block, pcl):
+    rng = np.random.default_rng(59)
+    p = _filled(rng, lengths, Hkv, d, code, block, F32)
+    blob, keep = _blob(rng, lengths, Hq, pcl, empty_head=1)
+    q = torch.from_numpy(rng.standard_normal((len(lengths), Hq, d))).float().to(DEV)
+    for at in (0, pcl - 1, pcl, 10 ** 6):
+        positions = [min(n - 1, at) for n in lengths]
+        O, lse, scratch = B.dam_cache_decode_attention(q, p.cache, _ints(positions), blob)
+        assert B.dam_poll_status(scratch) == 0
+        _check(p, q, positions, O, lse, keep, heads=sorted({0, 1, Hq // 2, Hq - 1}))
+
+
+@pytest.mark.parametrize("num_seqs", [48, 49, 104, 105, 222, 223])
+def test_attention_under_patterns_on_both_sides_of_every_split(num_seqs):
+    """Clusters of 8, 4 and 2 blocks, and one block: the last number of sequences of each and the first of the next."""
+    rng = np.random.default_rng(num_seqs)
+    p = _filled(rng, [200] * num_seqs, 1, 64, "int8", 16, BF16)
+    blob, keep = _blob(rng, [200] * num_seqs, 2, 96)
+    q = torch.from_numpy(rng.standard_normal((num_seqs, 2, 64))).float().to(BF16).to(DEV)
+    positions = [int(x) for x in rng.integers(0, 200, size=num_seqs)]
+    O, lse, scratch = B.dam_cache_decode_attention(q, p.cache, _ints(positions), blob)
+    assert B.dam_poll_status(scratch) == 0
+    _check(p, q, positions, O, lse, keep)
