@@ -76,8 +76,8 @@ _ARGS = {"dam_status_string": "i", "dam_mask_sizes": "ppippp", "dam_build_masks"
          "dam_prefill_host": "pppppippppp", "dam_build_masks_static": "pppppzp", "dam_selftest_bounded_wait": "pzup",
          "dam_decode_attention": "ppppppifpppzp", "dam_sparse_attention_rows": "pppppiifpppppzp",
          "dam_capture_accumulate": "ppippp", "dam_capture_average": "ppifppp", "dam_selftest_device_table": "pipp",
-         "dam_cache_sizes": "pipp", "dam_cache_write": "ppppppzp", "dam_cache_read": "ppppppzp",
-         "dam_cache_decode_attention": "ppppiifpppzp"}
+         "dam_cache_sizes": "pipp", "dam_cache_write": "pppppppp", "dam_cache_read": "pppppppp",
+         "dam_cache_decode_attention": "ppppiifppppp"}
 _CTYPE = {"p": ctypes.c_void_p, "z": ctypes.c_size_t, "i": ctypes.c_int32, "u": ctypes.c_uint32, "f": ctypes.c_float}
 
 _lib = None
@@ -138,13 +138,14 @@ _index_stream = _raw_stream if _raw_stream is not None else lambda index: torch.
 
 
 class _ByReference:
-    """`ref` is the reference to the structure `c`, made when c is set (every call passes it; byref takes as long as a check);
-    `index`: the CUDA device that cu_dev is on, -1 for none."""
+    """`ref` is the reference to the structure `c`, made when c is set (every call passes it; byref takes as long as a check), and
+    `address` its address; `index`: the CUDA device that cu_dev is on, -1 for none."""
 
     def __setattr__(self, name, value):
         object.__setattr__(self, name, value)
         if name == "c":
             object.__setattr__(self, "ref", ctypes.byref(value))
+            object.__setattr__(self, "address", ctypes.addressof(value))
         elif name == "cu_dev":
             object.__setattr__(self, "index", -1 if value is None else value.get_device())
 
@@ -164,11 +165,14 @@ class Shape(_ByReference):
             self.kv = _kv_rows(value)
 
 
+_BF16, _F32, _I32 = torch.bfloat16, torch.float32, torch.int32
+
+
 def _kv_rows(s: dam_shape_t):
-    """(shape of the K and V rows, strides of K, of V, dtype)"""
-    rows = (s.total_tokens, s.num_kv_heads, s.head_dim)
-    return (rows, (s.k_stride_tok, s.k_stride_head, 1), (s.v_stride_tok, s.v_stride_head, 1),
-            torch.bfloat16 if s.dtype == DAM_BF16 else torch.float32)
+    """(shape of the K and V rows, dtype, whether there are no gaps in them, strides of K, of V)"""
+    rows = T, H, d = (s.total_tokens, s.num_kv_heads, s.head_dim)
+    ks, vs = (s.k_stride_tok, s.k_stride_head, 1), (s.v_stride_tok, s.v_stride_head, 1)
+    return rows, _BF16 if s.dtype == DAM_BF16 else _F32, ks == vs == (H * d, d, 1), ks, vs
 
 
 def make_shape(cu_seqlens: Sequence[int], Hq: int, Hkv: int, d: int, dtype: torch.dtype, device=None,
@@ -437,9 +441,11 @@ def dam_cache_sizes(cache: Cache, Hq: int):
     return rows.value, scratch.value
 
 
+# The checks of the calls below are written for their usual case, a few attributes each: the host's part of a call is what bounds a
+# generation step of few tokens.  (Addresses as numbers, too: ctypes takes longer over a reference or a size_t.)
 def _per_sequence(x: torch.Tensor, n: int) -> int:
     """Pointer of an int32 tensor with one element per sequence."""
-    assert x.dtype is torch.int32 and x.numel() == n and x.is_contiguous()
+    assert x.dtype is _I32 and x.numel() == n and x.is_contiguous()
     return x.data_ptr()
 
 
@@ -456,7 +462,7 @@ def _check_rows(tokens: "Shape", K: torch.Tensor, V: torch.Tensor):
     """ValueError unless the rows that `tokens` describes lie inside K and V where K and V have them: K, V [tokens, heads,
     head_dim] or longer, or [heads, tokens, head_dim], with the strides of `tokens`; or flattened in another way (their last
     element is no further than K's and V's own).  The calls compare the usual case, the very shape, by themselves."""
-    tokens.kv = rows, *strides, dtype = _kv_rows(tokens.c)
+    tokens.kv = rows, dtype, _, *strides = _kv_rows(tokens.c)
     T, H, d = rows
     for name, x, (st, sh, _) in zip("KV", (K, V), strides):
         if T == 0:
@@ -483,13 +489,15 @@ def dam_cache_write(K: torch.Tensor, V: torch.Tensor, tokens: Shape, cache: Cach
     index = K.get_device()
     if scratch is None:
         scratch = _alloc(256, K.device)
-    rows, ks, vs, dtype = tokens.kv
-    if not (K.shape == rows and V.shape == rows and K.stride() == ks and V.stride() == vs and K.dtype is dtype and V.dtype is dtype):
+    rows, dtype, dense, ks, vs = tokens.kv
+    if not (K.shape == rows and V.shape == rows and K.dtype is dtype and V.dtype is dtype
+            and (K.is_contiguous() and V.is_contiguous() if dense else K.stride() == ks and V.stride() == vs)):
         _check_rows(tokens, K, V)
     if not (V.get_device() == index == scratch.get_device() and tokens.index == index == cache.index >= 0
             and (at is None or starts.get_device() == index)):
         _check_device(index, K=K, V=V, scratch=scratch, tokens=tokens, cache=cache, starts=starts)
-    rc = lib().dam_cache_write(K.data_ptr(), V.data_ptr(), tokens.ref, at, cache.ref, scratch.data_ptr(), scratch.numel(), _index_stream(index))
+    rc = (_lib or lib()).dam_cache_write(K.data_ptr(), V.data_ptr(), tokens.address, at, cache.address, scratch.data_ptr(), scratch.numel(),
+                                         _index_stream(index))
     if rc:
         _check(rc, "dam_cache_write")
     return scratch
@@ -505,16 +513,18 @@ def dam_cache_read(cache: Cache, tokens: Shape, starts: Optional[torch.Tensor] =
     if scratch is None:
         scratch = _alloc(256, cache.cu_dev.device)
     if K is None or V is None:
-        shape, ks, vs, dtype = _kv_rows(tokens.c)
-        rows = [torch.empty_strided(shape, strides, device=cache.cu_dev.device, dtype=dtype) for strides in (ks, vs)]
+        shape, dtype, _, *strides = _kv_rows(tokens.c)
+        rows = [torch.empty_strided(shape, x, device=cache.cu_dev.device, dtype=dtype) for x in strides]
         K, V = K if K is not None else rows[0], V if V is not None else rows[1]
-    rows, ks, vs, dtype = tokens.kv
-    if not (K.shape == rows and V.shape == rows and K.stride() == ks and V.stride() == vs and K.dtype is dtype and V.dtype is dtype):
+    rows, dtype, dense, ks, vs = tokens.kv
+    if not (K.shape == rows and V.shape == rows and K.dtype is dtype and V.dtype is dtype
+            and (K.is_contiguous() and V.is_contiguous() if dense else K.stride() == ks and V.stride() == vs)):
         _check_rows(tokens, K, V)
     if not (K.get_device() == V.get_device() == index == scratch.get_device() and tokens.index == index >= 0
             and (at is None or starts.get_device() == index)):
         _check_device(index, K=K, V=V, scratch=scratch, tokens=tokens, starts=starts)
-    rc = lib().dam_cache_read(cache.ref, tokens.ref, at, K.data_ptr(), V.data_ptr(), scratch.data_ptr(), scratch.numel(), _index_stream(index))
+    rc = (_lib or lib()).dam_cache_read(cache.address, tokens.address, at, K.data_ptr(), V.data_ptr(), scratch.data_ptr(), scratch.numel(),
+                                        _index_stream(index))
     if rc:
         _check(rc, "dam_cache_read")
     return K, V, scratch
@@ -533,7 +543,7 @@ def dam_cache_decode_attention(q: torch.Tensor, cache: Cache, positions: torch.T
     that cannot take the result, and for a tensor on another device than q."""
     n, Hq, d = shape = q.shape
     dtype = q.dtype
-    assert shape == (cache.num_seqs, Hq, cache.head_dim) and q.is_contiguous() and (dtype is torch.bfloat16 or dtype is torch.float32)
+    assert shape == (cache.num_seqs, Hq, cache.head_dim) and q.is_contiguous() and (dtype is _BF16 or dtype is _F32)
     at = _per_sequence(positions, n)
     index = q.get_device()
     if scratch is None:
@@ -545,13 +555,13 @@ def dam_cache_decode_attention(q: torch.Tensor, cache: Cache, positions: torch.T
     if not (O.get_device() == lse.get_device() == index == scratch.get_device() and positions.get_device() == index == cache.index >= 0
             and (mask is None or mask.get_device() == index)):
         _check_device(index, q=q, O=O, lse=lse, scratch=scratch, positions=positions, cache=cache, mask=mask)
-    if not (O.dtype is dtype and O.is_contiguous() and O.numel() == n * Hq * d):
+    if not (O.dtype is dtype and O.is_contiguous() and O.shape == shape):
         _check_result(O, "O", n * Hq * d, dtype)
-    if not (lse.dtype is torch.float32 and lse.is_contiguous() and lse.numel() == n * Hq):
-        _check_result(lse, "lse", n * Hq, torch.float32)
-    rc = lib().dam_cache_decode_attention(q.data_ptr(), cache.ref, None if mask is None else mask.data_ptr(), at, Hq,
-                                          DAM_BF16 if dtype is torch.bfloat16 else DAM_F32, softmax_scale, O.data_ptr(), lse.data_ptr(),
-                                          scratch.data_ptr(), scratch.numel(), _index_stream(index))
+    if not (lse.dtype is _F32 and lse.is_contiguous() and lse.numel() == n * Hq):
+        _check_result(lse, "lse", n * Hq, _F32)
+    rc = (_lib or lib()).dam_cache_decode_attention(q.data_ptr(), cache.address, None if mask is None else mask.data_ptr(), at, Hq,
+                                                    DAM_BF16 if dtype is _BF16 else DAM_F32, softmax_scale, O.data_ptr(), lse.data_ptr(),
+                                                    scratch.data_ptr(), scratch.numel(), _index_stream(index))
     if rc:
         _check(rc, "dam_cache_decode_attention")
     return O, lse, scratch
