@@ -8,9 +8,12 @@
 // instruction's tile, so nothing of it is padding where a group has 8 heads.  fp16 operands: q is scaled by a power of two so
 // that its largest element lies in [2^14, 2^15) (a bf16 q is then exact wherever it matters), and the weights, probability times sV,
 // are held in units of their own for every head: a power of two that puts the largest weight of the head so far between 2^11 and
-// 2^15.  An fp32 q and its weights are each the sum of two fp16 numbers (22 bits), at the price of twice the instructions.  What fp16's
-// last step of 2^-24 drops of a weight is 2^-36 of the head's largest, and 2^-47 where there is a second number, which is held 2^11
-// times larger than the first: a key that the head does not keep, or that has no probability, costs the others nothing however large its V is.
+// 2^15.  A weight of a bf16 query is one fp16 number, 11 bits under a result of 8: the result's error against 64 bits grows by 1 to
+// 2 % (1.69e-3 -> 1.72e-3, one sequence of 8000 tokens), and for more than four heads a second number would double the second
+// product's instructions.  An fp32 q and its weights are each the sum of two fp16 numbers (22 bits), at the price of twice the
+// instructions.  What fp16's last step of 2^-24 drops of a weight is 2^-36 of the head's largest, and 2^-47 where there is a second
+// number, which is held 2^11 times larger than the first: a key that the head does not keep, or that has no probability, costs the
+// others nothing however large its V is.
 //
 // A warp works on slices of 16 keys (two at a time where keys are contiguous: two independent chains of instructions), brought to
 // shared memory by asynchronous copies ahead of their use, and keeps a running softmax and its share of O^T of its own; the warps of
@@ -19,8 +22,9 @@
 // registers.
 //
 // Bound by HBM: 2 d bytes and two scales per key and KV head are read once.  64 sequences of 16k to 32k tokens (8 KV heads of 128,
-// int8): 500 to 560 us, 5.8 to 6.6 TB/s of codes and scales; one of 64k to 128k tokens 37 us with its 7 us of beginning and end.
-// A slice costs about 320 warp instructions, a third of them the conversion of its codes (int8: exclusive or, byte permutation and
+// int8): 515 to 590 us by box and by how the batch repeats, 5.5 to 6.2 TB/s of codes and scales; one of 64k to 128k tokens 33 to 39 us with
+// its 7 us of beginning and end.
+// A slice costs about 330 warp instructions, a third of them the conversion of its codes (int8: exclusive or, byte permutation and
 // one subtraction for two codes; e4m3: one conversion), and 175 cycles of its SM's share of the bandwidth: with the copies issued
 // by the lanes (cp.async, 600 instructions in all) the same batch took 820 us.
 #include <cooperative_groups.h>
@@ -951,9 +955,9 @@ cache_decode_short_kernel(const __grid_constant__ CUtensorMap kmap, const __grid
 // ---- the keys of the stored patterns ------------------------------------------------------------
 // As decode_group_kernel (dam_decode_mma.cu): one block, or a cluster of two to eight, per (sequence, KV head, group of 8 heads)
 // expands the patterns of its heads into one key list and deals its slices of 16 keys to the warps.  Rows are gathered by cp.async.
-// 64 sequences of 16k to 32k tokens, window 1024 (440 keys a list, 48 MB): 20 us, of which 4 until the first rows are asked for
+// 64 sequences of 16k to 32k tokens, window 1024 (440 keys a list, 48 MB): 19 us, of which 4 until the first rows are asked for
 // (header and position, sequence record, words: three dependent reads; then the list), 10 of gathering, 1 to 2 of joining.  One
-// sequence of 8000: 7.2 us.
+// sequence of 8000: 7.4 us.
 constexpr int kMWarps = 5, kMStages = 2, kMBlocks = 4;
 constexpr int kScales = 2 * kSlice * 4;         // bytes of the scales of a slice
 
