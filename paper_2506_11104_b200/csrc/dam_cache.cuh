@@ -133,8 +133,9 @@ struct Coder {
         for (int k = 0; k < 8; ++k) {
           const float q = t[k] - kMagic, twice = 2.f * fmaf(-q, s, x[k]);
           const bool odd = (__float_as_uint(t[k]) & 1u) != 0;
-          if (twice > s || (twice == s && odd)) t[k] += 1.f;
-          else if (twice < -s || (twice == -s && odd)) t[k] -= 1.f;
+          const float far = fabsf(twice);
+          // (the next float is the next integer there)
+          if (far > s || (far == s && odd)) t[k] = __uint_as_float(__float_as_uint(t[k]) + (twice < 0.f ? -1 : 1));
         }
       }
 #pragma unroll
