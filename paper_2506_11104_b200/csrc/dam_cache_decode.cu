@@ -69,14 +69,9 @@ __device__ __forceinline__ uint32_t pack_half2(float lo, float hi) {
   const __half2 h = __floats2half2_rn(lo, hi);
   return *reinterpret_cast<const uint32_t*>(&h);
 }
-// The second number of a weight is held kLow times larger (it is at most 2^4, half a step of 2^15), under codes divided by kLow: exact,
-// int8's step of 2^-11 and e4m3's of 2^-20 are fp16 numbers.
+// The second number of a weight is held kLow times larger (it is at most 2^4, half a step of 2^15), and so are its products, in columns
+// or in an accumulator of their own.
 constexpr float kLow = 2048.f;
-__device__ __forceinline__ uint32_t low_codes(uint32_t h) {
-  uint32_t r;
-  asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(h), "r"(0x10001000u));      // (2^-11, twice)
-  return r;
-}
 // four codes in memory order -> two operand registers (codes 0, 1 and codes 2, 3)
 template <int CODE>
 __device__ __forceinline__ void codes_to_half(uint32_t w, uint32_t* h) {
@@ -361,7 +356,13 @@ struct WarpState {
           codes_to_half<CODE>(__byte_perm(vw[2][i], vw[3][i], sel), b);
           const int u = 2 * i + k;
           mma_f16(o[u], a[0], a[1], b[0], b[1], pb[n][0], pb[n][1]);
-          if constexpr (kSplit) mma_f16(o[u], low_codes(a[0]), low_codes(a[1]), low_codes(b[0]), low_codes(b[1]), pl[n][0], pl[n][1]);
+          if constexpr (kSplit) {
+            // (codes divided by kLow instead, four multiplications of halves: 64 x 1000 tokens of 64 heads of 128 38.6 us, this 33.9)
+            float low[4] = {};
+            mma_f16(low, a[0], a[1], b[0], b[1], pl[n][0], pl[n][1]);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[u][e] = fmaf(low[e], 1.f / kLow, o[u][e]);
+          }
         }
       }
     }
